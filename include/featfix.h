@@ -418,6 +418,120 @@ ff_status ff_ctx_trace(ff_ctx* c, void* buf, size_t bytes);
 ff_status ff_rel_l1(const ff_model_desc* m, const void* a, const void* b, float eps, float* rel, void* ws,
                     size_t ws_bytes, ff_stream_t stream);
 
+/* ---------------------------------------------------------------- 8-bit operands
+ * The text tower that forms txt and cond, and linears in 8 bits, beside the denoiser (the
+ * paper leaves both to the backbone, Sec. 3.1).  An 8-bit tensor holds OCP e4m3 values (fn:
+ * no infinities, largest 448) and an fp32 scale for each block:
+ *     s = max(largest |v| of the block, 2^-100) / 448,   q = e4m3(v * (1 / s)),   v ~ s q,
+ * in fp32, rounded to nearest even; an all-zero block has zeros.  A NaN stays NaN in its
+ * place, and an infinity makes its block's values NaN.  Blocks are
+ *   rows:     128 columns of one row (activations); the scale of row r and column block b is
+ *             qs[b * qs_ld + r], so that the rows of a block lie together; qs_ld >= rows;
+ *   squares:  128 rows x 128 columns (weights, laid out once); the scale of row block a and
+ *             column block b is qs[a * qs_ld + b], qs_ld >= ceil(C / 128).
+ * The last block of a direction holds what is left.  All pitches count elements.
+ *
+ * The rules of this section and the next, beside those above: rows, M, n_q of 0 queue
+ * nothing and succeed (checked like any other call); a buffer's rows lie at its own pitch,
+ * and what lies between, behind the last row or in other columns is neither read nor
+ * written; outputs overlap no input or other output unless a call says so; the stream and
+ * all buffers belong to the current device; nothing is kept between calls, so calls on
+ * several streams may share inputs, and need workspaces of their own.  Calls may be captured
+ * into a graph; one captured call, or ones that follow each other, may share a workspace. */
+#define FF_Q8_BLOCK 128
+
+/* C % 8 == 0, C >= 8, rows >= 0; x_row, q_row >= C and multiples of 8; block_rows 1 (rows) or 128
+ * (squares).  dtype: of x. */
+typedef struct {
+  int32_t rows, C, dtype, block_rows;
+  int64_t x_row, q_row, qs_ld;
+} ff_quant_desc;
+
+/* q, qs <- x in 8 bits (x [rows, C]).
+ * Errors: FF_E_NULL, FF_E_DTYPE, FF_E_RANGE (block_rows), FF_E_SHAPE (sizes, pitches,
+ * alignment, overlap), FF_E_HIP. */
+ff_status ff_quant_q8(const ff_quant_desc* d, const void* x, void* q, float* qs, ff_stream_t stream);
+
+/* dtype: of x, resid, gain, sum and y.  8 <= C <= 16384, C % 8 == 0, rows >= 0; the pitches of the
+ * tensors that are passed >= C and multiples of 8, qs_ld >= rows; eps > 0. */
+typedef struct {
+  int32_t rows, C, dtype;
+  float eps;
+  int64_t x_row, resid_row, sum_row, y_row, q_row, qs_ld;
+} ff_norm_desc;
+
+/* Root-mean-square norm of the rows of x [rows, C], or of the residual stream x + resid:
+ *     t = resid ? round_dtype(x + resid) : x;   v = t * (1 / sqrt(mean(t^2) + eps)) * gain
+ * (fp32; gain NULL: ones).  sum (NULL unless resid is given; may be x or resid itself, at the
+ * same pitch) receives t, y (may be NULL) v rounded to dtype, and q with qs (NULL together) v in
+ * 8 bits, blocks of rows, from the unrounded v.  At least one of y and q.
+ * Errors: FF_E_NULL, FF_E_DTYPE, FF_E_RANGE (eps), FF_E_SHAPE, FF_E_HIP. */
+ff_status ff_rms_norm_q8(const ff_norm_desc* d, const void* x, const void* resid, const void* gain, void* sum,
+                         void* y, void* q, float* qs, ff_stream_t stream);
+
+/* M >= 0, N >= 8, N % 8 == 0, K >= 16, K % 16 == 0; a_row, w_row >= K, multiples of 16; out_row (and
+ * resid_row with resid) >= N, multiples of 8; as_ld >= M; ws_ld >= ceil(K / 128); 256 rows of a or
+ * w, and all scales of either, within 2^31 bytes.  out_dtype: of bias, resid and out. */
+typedef struct {
+  int32_t M, N, K, out_dtype;
+  int32_t gelu;           /* 1: GELU (tanh form) on the product with its bias, 0: none */
+  int64_t a_row, w_row, out_row, resid_row, as_ld, ws_ld;
+} ff_gemm_q8_desc;
+
+/* out [M, N] <- act(A W^T + bias) + resid, A [M, K] in 8 bits with scales a_s (blocks of rows),
+ * W [N, K] with scales w_s (squares):
+ *     (A W^T)[m, n] = sum_b a_s[b, m] w_s[n / 128, b] sum_{k in block b} a[m, k] w[n, k],
+ * sums in fp32, one rounding to out_dtype.  bias [N] and resid [M, N] may be NULL; out may be
+ * resid itself at the same pitch.  ws: at least ff_gemm_q8_workspace_bytes(d) bytes (NULL if
+ * that is 0; it is for most shapes: only few rows on a long K need one).
+ * Errors: FF_E_NULL, FF_E_DTYPE, FF_E_RANGE (gelu), FF_E_SHAPE, FF_E_WORKSPACE, FF_E_HIP. */
+size_t ff_gemm_q8_workspace_bytes(const ff_gemm_q8_desc* d);   /* 0 also for an invalid descriptor */
+ff_status ff_gemm_q8(const ff_gemm_q8_desc* d, const void* a, const float* a_s, const void* w, const float* w_s,
+                     const void* bias, const void* resid, void* out, void* ws, size_t ws_bytes, ff_stream_t stream);
+
+/* ---------------------------------------------------------------- attention over spans
+ * Softmax attention of n_q queries over n_k keys per sample (the blocks' own attention, Eq. 1,
+ * sees every key and has a key head per query head):
+ *     t_ij = scale q_i . k_j;   cap > 0: t_ij <- cap tanh(t_ij / cap);   t_ij <- t_ij + bias
+ *     out_i = sum_j softmax_j(t_ij) v_j   over the keys j that query i sees.
+ * H query heads share H_kv key / value heads: head h reads key head h / (H / H_kv).  Element
+ * (b, i, h, e) of q lies at b q_batch + i q_row + h q_head + e, and so on for k, v and out
+ * (a projection's [B, N, 3, H, d] result, a cache with room behind its rows, or one sample's
+ * keys for all (batch 0) are strides).
+ * spans: which keys a query sees.  int32 [B, n_q, n_spans, 2] (span_batch elements between
+ * samples, 0 to share): query i sees the keys of [first, end) of each of its 1 or 2 spans, cut
+ * to [0, n_k); a key in both counts once.  n_spans 0 (spans NULL): all keys.  With the spans a
+ * query's keys are any document of a packed row (its first and end), a causal or prefix mask
+ * (end = max(i + 1, prefix)), a window, the filled part of a cache, or the joint sequence
+ * [txt ; img] with padded text (two spans).  A query with no key, or all of whose scores are
+ * -inf, gets zeros.  What a key or value row holds (infinities, NaN) has no effect on a query
+ * that does not see it.
+ * bias: FF_BIAS_NONE; FF_BIAS_SLOPE: - bias[h] |j - p_i|, fp32 [H]; FF_BIAS_TABLE:
+ * bias[h][min(max(j - p_i, -R), R) + R], fp32 [H, 2 R + 1], R = bias_reach.  p_i = pos[b] + i, pos
+ * int32 [B] (NULL: zeros; cut to +-2^30), is where query i stands among the keys.
+ * Scores, statistics and sums are fp32; in bf16 the probabilities enter the product with v
+ * rounded to bf16.  ws: at least ff_attention_workspace_bytes(d) bytes (NULL if that is 0:
+ * only few queries on many keys, whose keys are split, need one). */
+enum { FF_BIAS_NONE = 0, FF_BIAS_SLOPE = 1, FF_BIAS_TABLE = 2 };
+
+/* B >= 1, H % H_kv == 0, d in [8, 128] and d % 8 == 0, n_q, n_k >= 0 (and n_q H B, n_k below 2^30);
+ * strides non-negative multiples of 8, out's rows apart from each other; 64 key or value rows
+ * within 2^31 bytes; scale > 0, cap >= 0, both finite; 0 <= bias_reach <= 2^20; n_spans 0, 1 or 2. */
+typedef struct {
+  int32_t dtype, B, H, H_kv, d, n_q, n_k;
+  int32_t bias_kind, bias_reach, n_spans;
+  int64_t q_batch, q_row, q_head, k_batch, k_row, k_head, v_batch, v_row, v_head;
+  int64_t o_batch, o_row, o_head, span_batch;
+  float scale, cap;
+} ff_attn_desc;
+
+/* Errors: FF_E_NULL, FF_E_DTYPE, FF_E_RANGE (scale, cap, bias, n_spans), FF_E_SHAPE,
+ * FF_E_WORKSPACE, FF_E_HIP. */
+size_t ff_attention_workspace_bytes(const ff_attn_desc* d);   /* 0 also for an invalid descriptor */
+ff_status ff_attention(const ff_attn_desc* d, const void* q, const void* k, const void* v, const float* bias,
+                       const int32_t* pos, const int32_t* spans, void* out, void* ws, size_t ws_bytes,
+                       ff_stream_t stream);
+
 /* ---------------------------------------------------------------- profiling
  * Optional tracing of a context's launches (Sec. 4 reports latency per arm; this
  * attributes it to kernels).  While enabled, ff_denoise_step brackets every kernel

@@ -27,12 +27,16 @@ FF_STEP_REFRESH, FF_STEP_CACHED = 0, 1
 FF_ACT_EXACT, FF_ACT_DRAFT, FF_ACT_SITE, FF_ACT_RECOMPUTE = 0, 1, 2, 3
 FF_MAX_K, FF_MAX_SLOTS, FF_TEMB_DIM = 3, 8, 256
 FF_NOALLOC_VERIFY_MAX_B = 16
+FF_Q8_BLOCK = 128
+FF_BIAS_NONE, FF_BIAS_SLOPE, FF_BIAS_TABLE = 0, 1, 2
 
 # every symbol include/featfix.h declares
 EXPORTED = ("ff_abi_version", "ff_last_error", "ff_plan_build", "ff_plan_destroy", "ff_plan_export",
             "ff_cache_bytes", "ff_workspace_bytes", "ff_block_exact", "ff_cache_update",
             "ff_draft_forecast", "ff_verify_replace", "ff_verify_replace_noalloc", "ff_ctx_create", "ff_ctx_destroy",
             "ff_ctx_reset", "ff_get_counts", "ff_ctx_step_kinds", "ff_denoise_step", "ff_ctx_trace", "ff_hist_sum_bytes", "ff_ctx_hist_sums", "ff_cond_cache_bytes", "ff_ctx_cond_cache", "ff_rel_l1",
+            "ff_quant_q8", "ff_rms_norm_q8", "ff_gemm_q8_workspace_bytes", "ff_gemm_q8",
+            "ff_attention_workspace_bytes", "ff_attention",
             "ff_ctx_profile", "ff_ctx_profile_read")
 PROF_CLASSES = ("gemm", "attn", "norm", "gemv", "draft", "verify", "cache", "other")
 
@@ -79,6 +83,28 @@ class ff_counts(C.Structure):
     def as_dict(self):
         return {"n_full_refresh": self.n_full_refresh, "n_paid_checks": self.n_paid_checks,
                 "n_forwarded": self.n_forwarded, "n_recomputed": self.n_recomputed}
+
+
+class ff_quant_desc(C.Structure):
+    _fields_ = [(f, C.c_int32) for f in ("rows", "C", "dtype", "block_rows")] + \
+               [(f, C.c_int64) for f in ("x_row", "q_row", "qs_ld")]
+
+
+class ff_norm_desc(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("C", C.c_int32), ("dtype", C.c_int32), ("eps", C.c_float)] + \
+               [(f, C.c_int64) for f in ("x_row", "resid_row", "sum_row", "y_row", "q_row", "qs_ld")]
+
+
+class ff_gemm_q8_desc(C.Structure):
+    _fields_ = [(f, C.c_int32) for f in ("M", "N", "K", "out_dtype", "gelu")] + \
+               [(f, C.c_int64) for f in ("a_row", "w_row", "out_row", "resid_row", "as_ld", "ws_ld")]
+
+
+class ff_attn_desc(C.Structure):
+    _fields_ = [(f, C.c_int32) for f in ("dtype", "B", "H", "H_kv", "d", "n_q", "n_k", "bias_kind", "bias_reach",
+                                         "n_spans")] + \
+               [(f"{t}_{w}", C.c_int64) for t in "qkvo" for w in ("batch", "row", "head")] + \
+               [("span_batch", C.c_int64), ("scale", C.c_float), ("cap", C.c_float)]
 
 
 class ff_prof_stat(C.Structure):
@@ -132,6 +158,12 @@ def lib():
             "ff_ctx_cond_cache": (i32, [vp, vp, sz]),
             "ff_rel_l1": (i32, [P(ff_model_desc), vp, vp, f32, vp, vp, sz, vp]),
             "ff_denoise_step": (i32, [vp, i32, vp, vp, vp, vp, vp]),
+            "ff_quant_q8": (i32, [P(ff_quant_desc), vp, vp, vp, vp]),
+            "ff_rms_norm_q8": (i32, [P(ff_norm_desc)] + [vp] * 8),
+            "ff_gemm_q8_workspace_bytes": (sz, [P(ff_gemm_q8_desc)]),
+            "ff_gemm_q8": (i32, [P(ff_gemm_q8_desc)] + [vp] * 8 + [sz, vp]),
+            "ff_attention_workspace_bytes": (sz, [P(ff_attn_desc)]),
+            "ff_attention": (i32, [P(ff_attn_desc)] + [vp] * 8 + [sz, vp]),
             "ff_ctx_profile": (i32, [vp, i32]),
             "ff_ctx_profile_read": (i32, [vp, P(ff_prof_stat)]),
         }
@@ -293,6 +325,31 @@ def ff_rel_l1(model, a, b, eps, rel, ws, ws_bytes, stream=0):
 
 def ff_denoise_step(ctx, step, x, cond, txt, audit, stream=0):
     return check(lib().ff_denoise_step(ctx, step, x, cond, txt, audit, stream))
+
+
+# Operators on 8-bit operands and attention over spans (addresses or None).
+def ff_quant_q8(desc, x, q, qs, stream=0):
+    return check(lib().ff_quant_q8(C.byref(desc), x, q, qs, stream))
+
+
+def ff_rms_norm_q8(desc, x, resid, gain, sum, y, q, qs, stream=0):
+    return check(lib().ff_rms_norm_q8(C.byref(desc), x, resid, gain, sum, y, q, qs, stream))
+
+
+def ff_gemm_q8_workspace_bytes(desc):
+    return lib().ff_gemm_q8_workspace_bytes(C.byref(desc))
+
+
+def ff_gemm_q8(desc, a, a_s, w, w_s, bias, resid, out, ws, ws_bytes, stream=0):
+    return check(lib().ff_gemm_q8(C.byref(desc), a, a_s, w, w_s, bias, resid, out, ws, ws_bytes, stream))
+
+
+def ff_attention_workspace_bytes(desc):
+    return lib().ff_attention_workspace_bytes(C.byref(desc))
+
+
+def ff_attention(desc, q, k, v, bias, pos, spans, out, ws, ws_bytes, stream=0):
+    return check(lib().ff_attention(C.byref(desc), q, k, v, bias, pos, spans, out, ws, ws_bytes, stream))
 
 
 def ff_ctx_profile(ctx, enable):

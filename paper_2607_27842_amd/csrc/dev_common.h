@@ -126,6 +126,36 @@ __device__ __forceinline__ float wave_max(float v) {
   return v;
 }
 
+// Sum over the 64 lanes of a wavefront for the row statistics, every lane receiving it, in
+// a fixed order: within each row of 16 lanes by DPP moves (xor 1, xor 2, then the 8- and
+// 16-lane mirrors, which pair each partial sum with one covering the other lanes), then the
+// four rows by the gfx950 row-pair and half-wavefront swaps (v_permlane16_swap,
+// v_permlane32_swap), each adding the even-row (lower-half) value to the odd-row
+// (upper-half) one in every lane.  No step goes through the LDS crossbar (the DPP steps
+// alone took about 0.2 us off a LayerNorm launch at DiT-XL/2 size against the butterfly of
+// six crossbar shuffles).
+template <int CTL>
+__device__ __forceinline__ float dpp_mov(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), CTL, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float row_sum(float v) {
+  v += dpp_mov<0xB1>(v);    // quad_perm [1, 0, 3, 2]
+  v += dpp_mov<0x4E>(v);    // quad_perm [2, 3, 0, 1]
+  v += dpp_mov<0x141>(v);   // row_half_mirror
+  v += dpp_mov<0x140>(v);   // row_mirror
+  const auto r16 = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(r16[0]) + __uint_as_float(r16[1]);
+  const auto r32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r32[0]) + __uint_as_float(r32[1]);
+}
+// Largest value over each row of 16 lanes, every lane of the row receiving it
+__device__ __forceinline__ float max16(float v) {
+  v = fmaxf(v, dpp_mov<0xB1>(v));
+  v = fmaxf(v, dpp_mov<0x4E>(v));
+  v = fmaxf(v, dpp_mov<0x141>(v));
+  return fmaxf(v, dpp_mov<0x140>(v));
+}
+
 inline int cdiv(long a, long b) { return (int)((a + b - 1) / b); }
 
 // ---------------------------------------------------------------- LDS reads and DMA by hand

@@ -15,17 +15,16 @@
 #include <vector>
 
 #include "featfix.h"
+#include "host.h"
 #include "kernels.h"
 
 using namespace ff;
 
 namespace ff {
+
 thread_local LaunchEvents g_launch_events;
-}
 
-namespace {
-
-thread_local char g_err[512] = "";
+static thread_local char g_err[512] = "";
 
 ff_status fail(ff_status code, const char* fmt, ...) {
   va_list ap;
@@ -41,11 +40,10 @@ ff_status ok() {
 ff_status hip_fail(hipError_t e, const char* where) {
   return fail(FF_E_HIP, "%s: %s", where, hipGetErrorString(e));
 }
-#define HIP_TRY(expr, where)              \
-  do {                                    \
-    hipError_t _e = (expr);               \
-    if (_e != hipSuccess) return hip_fail(_e, where); \
-  } while (0)
+
+}  // namespace ff
+
+namespace {
 
 constexpr size_t kAlign = 256;
 inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
@@ -66,8 +64,6 @@ struct Model {
   size_t es() const { return dsize(dtype); }
   size_t E() const { return (size_t)B * N * C; }
 };
-
-bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
 // the rotary embedding of the q / k norm kernel (axes 0: none)
 Rope rope_of(const Model& m) {

@@ -140,6 +140,59 @@ struct AttnArgs {
 };
 hipError_t attention(int dtype, const AttnArgs& a, hipStream_t s);
 
+// ---------------------------------------------------------------- 8-bit operands
+// e4m3 values with an fp32 scale per 128 columns of a row (scale of row r, block b at qs[b * qs_ld + r])
+// or per 128 x 128 square (qs[a * qs_ld + b]); include/featfix.h states the format.
+constexpr int kQBlock = 128;
+struct QuantArgs {
+  const void* x; int64_t x_row;
+  uint8_t* q; int64_t q_row;
+  float* qs; int64_t qs_ld;
+  int rows, C;
+};
+hipError_t quant_rows(int dtype, const QuantArgs& a, hipStream_t s);
+hipError_t quant_squares(int dtype, const QuantArgs& a, hipStream_t s);
+// t = round(x + resid) or x, v = t / sqrt(mean(t^2) + eps) * gain; sum <- t, y <- v, q <- v in 8 bits
+// (each where not NULL)
+constexpr int kNormMaxC = 16384;
+struct RmsArgs {
+  const void* x; int64_t x_row;
+  const void* resid; int64_t resid_row;
+  const void* gain;
+  void* sum; int64_t sum_row;
+  void* y; int64_t y_row;
+  uint8_t* q; int64_t q_row;
+  float* qs; int64_t qs_ld;
+  int rows, C; float eps;
+};
+hipError_t rms_norm_q8(int dtype, const RmsArgs& a, hipStream_t s);
+// out = act(sum_b a_s[b, m] w_s[n / 128, b] sum_{k in b} a[m, k] w[n, k] + bias) + resid
+struct GemmQ8Args {
+  const uint8_t* a; int64_t a_row; const float* a_s; int64_t as_ld;
+  const uint8_t* w; int64_t w_row; const float* w_s; int64_t ws_ld;
+  const void* bias; const void* resid; int64_t resid_row;   // in the output's type
+  void* out; int64_t out_row;
+  int M, N, K, gelu;
+  float* part;   // workspace: gemm_q8_workspace floats
+};
+size_t gemm_q8_workspace(int M, int N, int K);
+hipError_t gemm_q8(int out_dtype, const GemmQ8Args& a, hipStream_t s);
+
+// ---------------------------------------------------------------- attention over spans
+// Rows of a (sample, key head): row r is query r / G of query head hk * G + r % G.
+enum { BIAS_NONE = 0, BIAS_SLOPE = 1, BIAS_TABLE = 2 };
+struct AttnSpanArgs {
+  const void *q, *k, *v; void* out;
+  int64_t qb, qr, qh, kb, kr, kh, vb, vr, vh, ob, orow, oh;   // strides in elements
+  int B, H_kv, G, d, n_q, n_k;
+  float scale, cap;
+  int bias_kind, reach; const float* bias; const int32_t* pos;
+  const int32_t* spans; int n_spans; int64_t span_batch;
+  float* part;   // workspace: attention_span_workspace bytes
+};
+size_t attention_span_workspace(int dtype, int B, int H_kv, int G, int d, int n_q, int n_k);
+hipError_t attention_span(int dtype, const AttnSpanArgs& a, hipStream_t s);
+
 // ---------------------------------------------------------------- history / draft / verify
 // slot = round(h - u) (residual) or h (u == nullptr)
 hipError_t cache_update(int dtype, void* slot, const void* u, const void* h, size_t E, hipStream_t s);

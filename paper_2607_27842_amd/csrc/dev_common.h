@@ -98,6 +98,18 @@ template <> struct St<DT_F32> {
   }
 };
 
+// 8 elements at i: one 16-byte access for bf16, two for fp32
+template <int DT>
+__device__ __forceinline__ void load8(const void* p, size_t i, float* v) {
+  St<DT>::load(p, i, v);
+  if (St<DT>::V == 4) St<DT>::load(p, i + 4, v + 4);
+}
+template <int DT>
+__device__ __forceinline__ void store8(void* p, size_t i, const float* v) {
+  St<DT>::store(p, i, v);
+  if (St<DT>::V == 4) St<DT>::store(p, i + 4, v + 4);
+}
+
 __device__ __forceinline__ float silu_f(float x) { return x / (1.0f + expf(-x)); }
 
 // GELU, tanh form: 0.5 z (1 + tanh(u)) with u = sqrt(2/pi) (z + 0.044715 z^3).  Since

@@ -11,18 +11,6 @@ namespace {
 
 constexpr float kQFloor = 0x1p-100f;
 
-// 8 elements at i: one 16-byte access for bf16, two for fp32
-template <int DT>
-__device__ __forceinline__ void load8(const void* p, size_t i, float* v) {
-  St<DT>::load(p, i, v);
-  if (St<DT>::V == 4) St<DT>::load(p, i + 4, v + 4);
-}
-template <int DT>
-__device__ __forceinline__ void store8(void* p, size_t i, const float* v) {
-  St<DT>::store(p, i, v);
-  if (St<DT>::V == 4) St<DT>::store(p, i + 4, v + 4);
-}
-
 __device__ __forceinline__ float abs_max8(const float* v) {
   float m = fabsf(v[0]);
 #pragma unroll

@@ -7,6 +7,7 @@
 // block, chunks l / 16 and 4 + l / 16; which k stands where within the block does not matter as
 // long as both operands agree.
 #include "dev_common.h"
+#include <math.h>
 
 namespace ff {
 
@@ -19,6 +20,28 @@ __device__ __forceinline__ f32x4_t mfma_q8(i32x8_t a, i32x8_t b, f32x4_t c) {
 }
 __device__ __forceinline__ i32x8_t join(u32x4_t lo, u32x4_t hi) {
   return i32x8_t{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+}
+
+// fp32 outputs take exact products: e4m3 values widened to bf16 (exactly) on the bf16 MFMAs, whose
+// sums keep 24 bits (7.6e-8 of the result off on operands of widely spread exponents).  The 8-bit
+// MFMAs align a block's products to fewer bits (5.5e-5 off on the same operands, 1.5e-5 on normal
+// ones): far below a bf16 output's rounding of 2^-9, far above fp32's.
+__device__ __forceinline__ bf16x8_t widen(uint32_t lo, uint32_t hi) {
+  const bf16x2_t p[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true)};
+  return bf16x8_t{p[0][0], p[0][1], p[1][0], p[1][1], p[2][0], p[2][1], p[3][0], p[3][1]};
+}
+// one block's product of 16 weight rows (w0, w1) and 16 activation rows (x0, x1)
+template <int DT>
+__device__ __forceinline__ f32x4_t product(u32x4_t w0, u32x4_t w1, u32x4_t x0, u32x4_t x1) {
+  f32x4_t p = {0.f, 0.f, 0.f, 0.f};
+  if (DT == DT_BF16) return mfma_q8(join(w0, w1), join(x0, x1), p);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(w0[2 * h], w0[2 * h + 1]), widen(x0[2 * h], x0[2 * h + 1]), p, 0, 0, 0);
+    p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(w1[2 * h], w1[2 * h + 1]), widen(x1[2 * h], x1[2 * h + 1]), p, 0, 0, 0);
+  }
+  return p;
 }
 
 // 4 consecutive columns c.. of output row r (N % 8 == 0: in range as a whole)
@@ -41,36 +64,62 @@ __device__ __forceinline__ void finish4(const GemmQ8Args& a, int r, int c, f32x4
   else *reinterpret_cast<f32x4_t*>(reinterpret_cast<float*>(a.out) + o) = v;
 }
 
-// 16 x 16 tile, operands straight from memory, the 8 waves of a workgroup on interleaved blocks of K;
-// their sums meet in LDS in wave order.
-template <int DT>
-__global__ __launch_bounds__(512) void k_gemm_q8_dir(GemmQ8Args a) {
-  __shared__ f32x4_t red[8][64];
+// Few rows: 16 x 16 tile, operands straight from memory, the NW waves of a workgroup on interleaved
+// blocks of K with the loads of four blocks in flight; their sums meet in LDS in wave order.  Bound
+// by the latency of that one round of loads: M = 1, N = 8192, K = 2048 5.7 us (16.8 MB of weights).
+// Two or four 16-row tiles a workgroup, to read the weights once for them, were slower (M = 64, N =
+// 2048, K = 2048: 6.0 us against 7.1 with four): the rows come from the caches.
+template <int DT, int NW>
+__global__ __launch_bounds__(NW * 64) void k_gemm_q8_dir(GemmQ8Args a) {
+  constexpr int U = 4;
+  __shared__ f32x4_t red[NW][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, g = lane >> 4;
   const int tn = (a.N + 15) / 16, m0 = (blockIdx.x / tn) * 16, n0 = (blockIdx.x % tn) * 16;
   const int m = m0 + l16 < a.M ? m0 + l16 : m0, n = n0 + l16 < a.N ? n0 + l16 : n0;   // past the matrix: never stored
   const uint8_t* pa = a.a + (size_t)m * a.a_row;
   const uint8_t* pw = a.w + (size_t)n * a.w_row;
+  const float* sa = a.a_s + m;
   const float* sw = a.w_s + (size_t)(n0 / kQBlock) * a.ws_ld;
-  const f32x4_t z = {0.f, 0.f, 0.f, 0.f};
-  const u32x4_t zu = {0u, 0u, 0u, 0u};
-  f32x4_t acc = z;
+  f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
   const int nk = (a.K + kQBlock - 1) / kQBlock;
-  for (int b = wave; b < nk; b += 8) {
-    const int k0 = b * kQBlock + g * 16, k1 = k0 + 64;
-    const u32x4_t x0 = k0 < a.K ? *reinterpret_cast<const u32x4_t*>(pa + k0) : zu, x1 = k1 < a.K ? *reinterpret_cast<const u32x4_t*>(pa + k1) : zu;
-    const u32x4_t w0 = k0 < a.K ? *reinterpret_cast<const u32x4_t*>(pw + k0) : zu, w1 = k1 < a.K ? *reinterpret_cast<const u32x4_t*>(pw + k1) : zu;
-    const float s = a.a_s[(size_t)b * a.as_ld + m] * sw[b];
-    const f32x4_t p = mfma_q8(join(w0, w1), join(x0, x1), z);
+  for (int b0 = wave; b0 < nk; b0 += NW * U) {
+    u32x4_t x[U][2], w[U][2];
+    float s[U];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] = fmaf(p[e], s, acc[e]);
+    for (int u = 0; u < U; ++u) {
+      // blocks and chunks past K read the row's start, which is in bounds, and count for nothing
+      const int b = b0 + NW * u < nk ? b0 + NW * u : 0;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int k = b * kQBlock + g * 16 + h * 64, kk = k < a.K ? k : 0;
+        w[u][h] = *reinterpret_cast<const u32x4_t*>(pw + kk);
+        x[u][h] = *reinterpret_cast<const u32x4_t*>(pa + kk);
+      }
+      s[u] = sa[(size_t)b * a.as_ld] * sw[b];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (b0 + NW * u >= nk) break;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const bool in = (b0 + NW * u) * kQBlock + g * 16 + h * 64 < a.K;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {   // both operands, so that 0 * 0 is added
+          w[u][h][e] = in ? w[u][h][e] : 0u;
+          x[u][h][e] = in ? x[u][h][e] : 0u;
+        }
+      }
+      const f32x4_t p = product<DT>(w[u][0], w[u][1], x[u][0], x[u][1]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] = fmaf(p[e], s[u], acc[e]);
+    }
   }
   red[wave][lane] = acc;
   __syncthreads();
   if (wave) return;
 #pragma unroll
-  for (int i = 1; i < 8; ++i) {
+  for (int i = 1; i < NW; ++i) {
     const f32x4_t p = red[i][lane];
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[e] += p[e];
@@ -133,9 +182,9 @@ __device__ __forceinline__ void epilogue(const GemmQ8Args& a, int r0, int c0, co
 
 // Workgroup -> tile: workgroups go round-robin over the 8 XCDs, so every XCD gets a contiguous range
 // of tiles, in groups of 8 tile rows, whose operand rows its L2 then shares.
-__device__ __forceinline__ void tile_at(int tiles_m, int tiles_n, int& tm, int& tn) {
-  const int n = gridDim.x, full = n / 8 * 8;
-  const int id = (int)blockIdx.x < full ? (blockIdx.x % 8) * (full / 8) + blockIdx.x / 8 : blockIdx.x;
+__device__ __forceinline__ void tile_at(int wg, int n, int tiles_m, int tiles_n, int& tm, int& tn) {
+  const int full = n / 8 * 8;
+  const int id = wg < full ? (wg % 8) * (full / 8) + wg / 8 : wg;
   const int per = 8 * tiles_n, first = id / per * 8, size = min(tiles_m - first, 8), in = id % per;
   tm = __builtin_amdgcn_readfirstlane(first + in % size);
   tn = __builtin_amdgcn_readfirstlane(in / size);
@@ -184,7 +233,7 @@ __global__ __launch_bounds__(512) void k_gemm_q8_pp(GemmQ8Args a) {
   __shared__ __attribute__((aligned(1024))) char lds[kMain > kEpi ? kMain : kEpi];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int tm, tn;
-  tile_at((a.M + BM - 1) / BM, (a.N + BN - 1) / BN, tm, tn);
+  tile_at(blockIdx.x, gridDim.x, (a.M + BM - 1) / BM, (a.N + BN - 1) / BN, tm, tn);
   const int m0 = tm * BM, n0 = tn * BN;
   const int mw = wave >> 2, nw = wave & 3;
   const int nk = (a.K + kQBlock - 1) / kQBlock;   // >= 3 (host check)
@@ -229,9 +278,8 @@ __global__ __launch_bounds__(512) void k_gemm_q8_pp(GemmQ8Args a) {
     rdb[s] = lds0 + OFFB + (nw * 16 + fr) * RB + c;
   }
   const uint32_t rds = lds0 + OFFS + (mw * 128 + fr) * 4;
-  // scalar loads: a vector load would wait for the DMA before it
-  typedef const __attribute__((address_space(4))) float* scalar_ptr;
-  const scalar_ptr wsc = (scalar_ptr)(a.w_s + (size_t)min((n0 + nw * WN) / kQBlock, (a.N - 1) / kQBlock) * a.ws_ld);
+  const float* wsc = a.w_s + (size_t)min((n0 + nw * WN) / kQBlock, (a.N - 1) / kQBlock) * a.ws_ld;
+  float vsw = wsc[min(lane, nk - 1)];   // the weight's scales of 64 stages, one a lane
   u32x4_t fa[4], fb[2 * TN];
   float sw = 0.f;
   int kb = 0, st = 0, ca = 0, cb = 0;   // this stage's byte offset along K and number, and its buffers
@@ -290,7 +338,7 @@ __global__ __launch_bounds__(512) void k_gemm_q8_pp(GemmQ8Args a) {
     if (k1) FF_DMA(ra, voa[3], 3 * PC + oa, kb + RB);
     if (k2) FF_DMAS(st + 2);
     FF_ADD(3);
-    sw = wsc[st];
+    sw = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vsw), st & 63));
     wait_vm<pp_vm(TN, 0, LEFT)>();
     FF_MEM_END();
 #pragma unroll
@@ -360,9 +408,11 @@ __global__ __launch_bounds__(512) void k_gemm_q8_pp(GemmQ8Args a) {
       for (int u = 0; u < TN; ++u) vob[u] = cut ? 0x80000000u : vob[u];
     }
     stage(Int<2>{});
+    if ((st & 63) == 0) vsw = wsc[min(st + lane, nk - 1)];
   } while (--left);
   voa[3] = cut ? 0x80000000u : voa[3];
   stage(Int<1>{});
+  if ((st & 63) == 0) vsw = wsc[min(st + lane, nk - 1)];
   stage(Int<0>{});
   FF_ADD(3);
   if (wave < 4) asm volatile("s_barrier" ::: "memory");
@@ -378,22 +428,347 @@ __global__ __launch_bounds__(512) void k_gemm_q8_pp(GemmQ8Args a) {
 #endif
 }
 
+// ---------------------------------------------------------------- smaller grids, fp32 outputs
+// BM x BN tile, 8 waves in two groups of four; a group takes every second block of K for the whole tile
+// (2 x 2 waves), so that a fragment read feeds up to four MFMAs, and has its own ring of NS blocks.
+// Per block a wave has a memory slot (its fragments and scales, and the scaled addition of the former
+// block's sums) and a matrix slot (the DMA of the block NS ahead into the ring slot just read, then
+// the MFMAs), each ended by a barrier; the second group runs one slot behind, one wave of each group
+// per SIMD.  The two groups' sums meet in LDS: each finishes half of the rows.
+//
+template <int DT, int BM, int BN, int NS>
+__global__ __launch_bounds__(512) void k_gemm_q8_two(GemmQ8Args a, int splits) {
+#ifdef __HIP_DEVICE_COMPILE__   // the host pass needs the launch stub only
+  constexpr int TM = BM / 32, TN = BN / 32, WN = BN / 2, RB = kQBlock;
+  constexpr int STB = (BM + BN) * RB, SCB = BM < 256 ? 256 * ((BM + 63) / 64) : 1024;   // bytes of a block, of its rows' scales
+  constexpr int NA = BM / 32, NW = BN / 32, PER = NA + NW + 1;   // DMA instructions of a wave and block
+  constexpr int OFFS = 2 * NS * STB, kMain = OFFS + 2 * NS * SCB;
+  constexpr int HT = TM / 2, kXch = 8 * HT * TN * 1024, RE = HT > 1 ? 32 : 16, kEpi = kXch + 8 * RE * (WN + 4) * 4;
+  static_assert(TM % 2 == 0 && BN <= kQBlock, "halves of the rows; one weight scale a tile and block");
+  __shared__ __attribute__((aligned(1024))) char lds[kMain > kEpi ? kMain : kEpi];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int grp = wave >> 2, w = wave & 3, wr = w >> 1, wc = w & 1;
+  int tm, tn;
+  const int tiles = gridDim.x / splits, split = (int)blockIdx.x / tiles;
+  tile_at((int)blockIdx.x - split * tiles, tiles, (a.M + BM - 1) / BM, (a.N + BN - 1) / BN, tm, tn);
+  const int m0 = tm * BM, n0 = tn * BN;
+  // this workgroup's blocks of K: [kb0, kb0 + nb)
+  const int nk = (a.K + kQBlock - 1) / kQBlock, kb0 = (int)((long)nk * split / splits), nb = (int)((long)nk * (split + 1) / splits) - kb0;
+  const int mine = (nb - grp + 1) / 2, turns = (nb + 1) / 2;
+  auto rsrc = [](const void* p) __attribute__((always_inline)) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, 0x7fffff00u, 0x00020000);
+  };
+  __amdgpu_buffer_rsrc_t ra = rsrc(a.a + (size_t)m0 * a.a_row), rw = rsrc(a.w + (size_t)n0 * a.w_row), rs = rsrc(a.a_s + m0);
+  // rows past the matrix read the tile's first row (never stored); chunks of the last block past K are
+  // out of the resource's range and load zeros
+  uint32_t voa[NA], vow[NW];
+  unsigned cut = 0;
+#pragma unroll
+  for (int j = 0; j < NA + NW; ++j) {
+    const int R = (w * (j < NA ? NA : NW) + (j < NA ? j : j - NA)) * 8 + (lane >> 3);
+    const uint32_t ch = ((lane & 7) ^ ((R >> 1) & 7)) * 16;
+    if (j < NA) voa[j < NA ? j : 0] = (m0 + R < a.M ? (uint32_t)R * (uint32_t)a.a_row : 0u) + ch;
+    else vow[j < NA ? 0 : j - NA] = (n0 + R < a.N ? (uint32_t)R * (uint32_t)a.w_row : 0u) + ch;
+    if ((int)ch >= a.K - (nk - 1) * kQBlock) cut |= 1u << j;
+  }
+  const uint32_t vos = (uint32_t)min((w * 64 + lane) % BM, a.M - 1 - m0) * 4u, sstep = (uint32_t)a.as_ld * 4u;
+  constexpr int SW = BM / 64 > 0 ? BM / 64 : 1;   // waves whose scales differ; the others repeat them
+  char* const ring = lds + grp * NS * STB;
+  char* const sring = lds + OFFS + grp * NS * SCB;
+  auto issue1 = [&](int i, int slot, int j) __attribute__((always_inline)) {   // DMA j of the group's block i
+    const int kt = kb0 + 2 * i + grp, kb = kt * RB;
+    const unsigned c = kt == nk - 1 ? cut : 0u;
+    char* const dst = ring + slot * STB;
+    if (j < NA)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, FF_AS3(dst + (w * NA + j) * 1024), 16, voa[j < NA ? j : 0] | (c >> j & 1u) << 31, kb, 0, 0);
+    else if (j < NA + NW)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, FF_AS3(dst + BM * RB + (w * NW + j - NA) * 1024), 16,
+                                               vow[j < NA || j >= NA + NW ? 0 : j - NA] | (c >> j & 1u) << 31, kb, 0, 0);
+    else
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, FF_AS3(sring + slot * SCB + (w % SW) * 256), 4, vos, kt * sstep, 0, 0);
+  };
+  f32x4_t acc[TM][TN], part[TM][TN];
+  const f32x4_t z4 = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) acc[i][j] = part[i][j] = z4;
+  const int fr = lane & 15, fh = lane >> 4;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)((__attribute__((address_space(3))) const void*)lds);
+  uint32_t rda[2], rdw[2];
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    const uint32_t c = ((4 * s + fh) ^ (fr >> 1)) * 16, o = lds0 + grp * NS * STB;
+    rda[s] = o + (wr * (BM / 2) + fr) * RB + c;
+    rdw[s] = o + (BM + wc * WN + fr) * RB + c;
+  }
+  const uint32_t rds = lds0 + OFFS + grp * NS * SCB + (wr * (BM / 2) + fr) * 4;
+  // the weight's scales of the group's next 64 blocks, one a lane (a scalar load per block took up to a
+  // cache miss each 8 turns)
+  const float* wsc = a.w_s + (size_t)(n0 / kQBlock) * a.ws_ld;
+  float vsw = wsc[min(kb0 + grp + 2 * lane, nk - 1)];
+  u32x4_t fa[2 * TM], fw[2 * TN];
+  f32x2_t sv[HT];
+#pragma unroll
+  for (int t = 0; t < HT; ++t) sv[t] = f32x2_t{0.f, 0.f};
+  float sw = 0.f;
+  // the scales of the former block's sums, formed before sv's registers are read into again
+  float sp[TM];
+  auto scale = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      sp[i] = sv[i / 2][i % 2] * sw;
+      FF_TIE(sp[i]);
+    }
+  };
+  auto add = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(part[i][j][e], sp[i], acc[i][j][e]);
+        FF_TIE(acc[i][j]);
+      }
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < NS; ++i)
+    if (i < mine) {
+#pragma unroll
+      for (int j = 0; j < PER; ++j) issue1(i, i, j);
+    }
+  wait_vm<0>();
+  asm volatile("s_barrier" ::: "memory");
+  if (grp) asm volatile("s_barrier" ::: "memory");   // the second group runs one slot behind
+  int slot = 0;
+  auto turn = [&](int i, auto Mc) __attribute__((always_inline)) {
+    constexpr bool more = decltype(Mc)::value != 0;   // a block NS ahead is left
+    // memory slot
+    scale();
+    const uint32_t so = slot * STB;
+#pragma unroll
+    for (int t = 0; t < TN; ++t)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) fw[2 * t + s] = __builtin_bit_cast(u32x4_t, lds_rd128_off(rdw[s] + so, t * 16 * RB));
+#pragma unroll
+    for (int t = 0; t < TM; ++t)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) fa[2 * t + s] = __builtin_bit_cast(u32x4_t, lds_rd128_off(rda[s] + so, t * 16 * RB));
+#pragma unroll
+    for (int t = 0; t < HT; ++t)
+      asm volatile("ds_read2_b32 %0, %1 offset0:%2 offset1:%3" : "=v"(sv[t]) : "v"(rds + slot * SCB), "i"(32 * t), "i"(32 * t + 16) : "memory");
+    add();
+    sw = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vsw), i & 63));
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int t = 0; t < 2 * TN; ++t) FF_TIE(fw[t]);
+#pragma unroll
+    for (int t = 0; t < 2 * TM; ++t) FF_TIE(fa[t]);
+#pragma unroll
+    for (int t = 0; t < HT; ++t) FF_TIE(sv[t]);
+    asm volatile("s_barrier" ::: "memory");
+    // matrix slot: a DMA behind each MFMA
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(1);
+    if constexpr (DT == DT_BF16) {
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int t = 0; t < TM; ++t) {
+          part[t][j] = mfma_q8(join(fw[2 * j], fw[2 * j + 1]), join(fa[2 * t], fa[2 * t + 1]), z4);
+          if (more && j * TM + t < PER) {
+            __builtin_amdgcn_sched_barrier(0);
+            issue1(i + NS, slot, j * TM + t);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+    } else {
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        bf16x8_t xa[TM], xw[TN];
+#pragma unroll
+        for (int t = 0; t < TM; ++t) xa[t] = widen(fa[2 * t + s / 2][s % 2 * 2], fa[2 * t + s / 2][s % 2 * 2 + 1]);
+#pragma unroll
+        for (int t = 0; t < TN; ++t) xw[t] = widen(fw[2 * t + s / 2][s % 2 * 2], fw[2 * t + s / 2][s % 2 * 2 + 1]);
+#pragma unroll
+        for (int t = 0; t < TM; ++t)
+#pragma unroll
+          for (int j = 0; j < TN; ++j) part[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xw[j], xa[t], s == 0 ? z4 : part[t][j], 0, 0, 0);
+        if (more) {
+#pragma unroll
+          for (int j = s; j < (PER < TM * TN ? PER : TM * TN); j += 4) issue1(i + NS, slot, j);
+        }
+      }
+    }
+    if (more) {
+#pragma unroll
+      for (int j = TM * TN; j < PER; ++j) issue1(i + NS, slot, j);
+    }
+    __builtin_amdgcn_s_setprio(0);
+    __builtin_amdgcn_sched_barrier(0);
+    // the next block has landed; the ones after it may be on their way
+    wait_vm<more ? (NS - 1) * PER : 0>();
+    slot = slot == NS - 1 ? 0 : slot + 1;
+    asm volatile("s_barrier" ::: "memory");
+  };
+  int i = 0;
+  auto scales = [&]() __attribute__((always_inline)) {
+    if (i && (i & 63) == 0) vsw = wsc[min(kb0 + grp + 2 * (i + lane), nk - 1)];
+  };
+  for (; i < mine - NS; ++i) { scales(); turn(i, Int<1>{}); }
+  for (; i < mine; ++i) { scales(); turn(i, Int<0>{}); }
+  if (mine < turns) {   // the second group, one block short
+    asm volatile("s_barrier" ::: "memory");
+    asm volatile("s_barrier" ::: "memory");
+  }
+  scale();
+  add();
+  if (!grp) asm volatile("s_barrier" ::: "memory");
+  // every wave's LDS reads and DMA ended before the last barrier; each group finishes half of the rows
+  f32x4_t* const xch = reinterpret_cast<f32x4_t*>(lds) + lane;
+  f32x4_t fin[HT][TN];
+  auto half = [&](auto Gc) __attribute__((always_inline)) {
+    constexpr int G = decltype(Gc)::value;
+#pragma unroll
+    for (int t = 0; t < HT; ++t)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        xch[((wave * HT + t) * TN + j) * 64] = acc[(1 - G) * HT + t][j];
+        fin[t][j] = acc[G * HT + t][j];
+      }
+  };
+  if (grp) half(Int<1>{});
+  else half(Int<0>{});
+  __syncthreads();
+#pragma unroll
+  for (int t = 0; t < HT; ++t)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      const f32x4_t p = xch[(((wave ^ 4) * HT + t) * TN + j) * 64];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) fin[t][j][e] += p[e];
+    }
+  float* const stage = reinterpret_cast<float*>(lds + kXch) + wave * RE * (WN + 4);
+  const int r0 = m0 + wr * (BM / 2) + grp * HT * 16, c0 = n0 + wc * WN;
+  if (splits > 1) {   // bare sums for k_gemm_q8_join
+    GemmQ8Args p = a;
+    p.bias = p.resid = nullptr;
+    p.gelu = 0;
+    p.out = a.part + (size_t)split * a.M * a.N;
+    p.out_row = a.N;
+    epilogue<DT_F32, HT, TN>(p, r0, c0, fin, stage);
+  } else {
+    epilogue<DT, HT, TN>(a, r0, c0, fin, stage);
+  }
+#endif
+}
+
+// Joins the splits of K: 8 columns of a row a thread, the splits' sums in order
+template <int DT>
+__global__ __launch_bounds__(256) void k_gemm_q8_join(GemmQ8Args a, int splits) {
+  const int per = a.N / 8;
+  const size_t id = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (id >= (size_t)a.M * per) return;
+  const int r = (int)(id / per), c = (int)(id % per) * 8;
+  float v[8], x[8];
+  load8<DT_F32>(a.part, id * 8, v);
+  for (int i = 1; i < splits; ++i) {
+    load8<DT_F32>(a.part, (size_t)i * a.M * a.N + id * 8, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += x[e];
+  }
+  if (a.bias) {
+    load8<DT>(a.bias, c, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += x[e];
+  }
+  if (a.gelu) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = gelu_tanh_f(v[e]);
+  }
+  if (a.resid) {
+    load8<DT>(a.resid, (size_t)r * a.resid_row + c, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += x[e];
+  }
+  store8<DT>(a.out, (size_t)r * a.out_row + c, v);
+}
+
+// ---------------------------------------------------------------- choice
+enum Kind { kDir, kTwo64, kTwo128, kPP };
+struct Plan { Kind kind; int splits; };
+
+long tiles(long M, long N, long t) { return ((M + t - 1) / t) * ((N + t - 1) / t); }
+
+// The kernel of a shape by estimated time (us), fitted to 25 shapes of 1 to 4608 rows, N and K of 1152 to
+// 8192.  A tile of 64 x 64 takes 0.21 us per block of K while each CU has one, 0.5 with two on every CU;
+// 128 x 128 0.36 alone, 0.71 with all CUs (what the caches deliver); 256 x 256 1.95; fp32 outputs 1.5
+// times that.  Splits of K add the join: a launch, and writing and reading the partial sums.
+//   N 8192 K 2048, M = 16: k_gemm_q8_dir 7.1 us against 8.0 with 64 x 64 tiles; M = 64: 17.8 against 8.1
+//   M 128 N 2048 K 8192: 64 x 64 tiles 17.7 us, with 2 / 4 / 8 splits 14.2 / 12.4 / 14.7
+//   M 512 N 8192 K 2048: 128 x 128 14.9 us, 64 x 64 20.9, 256 x 256 31.9
+//   M 14566 N 8192 K 2048: 256 x 256 263 us, 128 x 128 322, 64 x 64 444
+Plan plan(int dt, int M, int N, int K) {
+  const int nk = (K + kQBlock - 1) / kQBlock;
+  const double slow = dt == DT_F32 ? 1.5 : 1.0;
+  Plan best{kTwo128, 1};
+  double least = 1e30;
+  auto take = [&](Kind k, int splits, double us) {
+    if (us < least) { least = us; best = Plan{k, splits}; }
+  };
+  if (M <= 256) {
+    const double t = (double)tiles(M, N, 16), chain = 0.4 * ((nk + 15) / 16);
+    take(kDir, 1, 2.5 + (t * nk * 0.45e-3 > chain ? t * nk * 0.45e-3 : chain));
+  }
+  for (int s = 1; s <= 8; s *= 2) {
+    if (s > 1 && nk / s < 8) break;
+    const double t = (double)tiles(M, N, 64) * s, nb = (double)nk / s;
+    const double main = t <= 256 ? (0.21 + 0.08 * t / 256) * nb : ceil(t / 512) * 0.5 * nb;
+    take(kTwo64, s, 3.5 + slow * main + (s > 1 ? 1.8 + s * (0.35 + 2.3e-6 * M * N) : 0.0));
+  }
+  const double t128 = (double)tiles(M, N, 128), t256 = (double)tiles(M, N, 256);
+  take(kTwo128, 1, 3.5 + slow * (t128 <= 256 ? 0.36 + 0.35 * t128 / 256 : ceil(t128 / 256) * 0.71) * nk);
+  if (dt == DT_BF16 && nk >= 3) take(kPP, 1, 4.0 + ceil(t256 / 256) * 1.95 * nk);
+  return best;
+}
+
+template <int DT>
+hipError_t launch_q8(const GemmQ8Args& a, hipStream_t s) {
+  const Plan p = plan(DT, a.M, a.N, a.K);
+  switch (p.kind) {
+    case kDir: {
+      // 16 waves where 8 would take their blocks in two rounds on a part of the CUs
+      const long t = tiles(a.M, a.N, 16);
+      if (a.K > 32 * kQBlock && t <= 256) FF_LAUNCH((k_gemm_q8_dir<DT, 16>), (unsigned)t, 1024, 0, s, a);
+      else FF_LAUNCH((k_gemm_q8_dir<DT, 8>), (unsigned)t, 512, 0, s, a);
+      break;
+    }
+    case kTwo64: FF_LAUNCH((k_gemm_q8_two<DT, 64, 64, 2>), (unsigned)(tiles(a.M, a.N, 64) * p.splits), 512, 0, s, a, p.splits); break;
+    case kTwo128: FF_LAUNCH((k_gemm_q8_two<DT, 128, 128, 2>), (unsigned)tiles(a.M, a.N, 128), 512, 0, s, a, 1); break;
+    case kPP:
+      if constexpr (DT == DT_BF16) FF_LAUNCH(k_gemm_q8_pp<4>, (unsigned)tiles(a.M, a.N, 256), 512, 0, s, a);
+      break;
+  }
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.splits == 1) return e;
+  const size_t wg = ((size_t)a.M * (a.N / 8) + 255) / 256;
+  FF_LAUNCH(k_gemm_q8_join<DT>, (unsigned)wg, 256, 0, s, a, p.splits);
+  return hipGetLastError();
+}
+
 }  // namespace
 
-size_t gemm_q8_workspace(int, int, int) { return 0; }
+size_t gemm_q8_workspace(int out_dtype, int M, int N, int K) {
+  if (M <= 0) return 0;
+  const int n = plan(out_dtype, M, N, K).splits;
+  return n > 1 ? (size_t)n * M * N * 4 : 0;
+}
 
 hipError_t gemm_q8(int out_dtype, const GemmQ8Args& a, hipStream_t s) {
   if (a.M <= 0) return hipSuccess;
-  if (out_dtype == DT_BF16 && a.K > 256 && a.M >= 512) {
-    const long wg = (long)((a.M + 255) / 256) * ((a.N + 255) / 256);
-    FF_LAUNCH(k_gemm_q8_pp<4>, (unsigned)wg, 512, 0, s, a);
-    return hipGetLastError();
-  }
-  const long wg = (long)((a.M + 15) / 16) * ((a.N + 15) / 16);
-  if (wg > 0x7fffffffL) return hipErrorInvalidValue;
-  if (out_dtype == DT_BF16) FF_LAUNCH(k_gemm_q8_dir<DT_BF16>, (unsigned)wg, 512, 0, s, a);
-  else FF_LAUNCH(k_gemm_q8_dir<DT_F32>, (unsigned)wg, 512, 0, s, a);
-  return hipGetLastError();
+  if (tiles(a.M, a.N, 16) > 0x7fffffffL) return hipErrorInvalidValue;
+  return out_dtype == DT_BF16 ? launch_q8<DT_BF16>(a, s) : launch_q8<DT_F32>(a, s);
 }
 
 }  // namespace ff

@@ -173,9 +173,9 @@ struct GemmQ8Args {
   const void* bias; const void* resid; int64_t resid_row;   // in the output's type
   void* out; int64_t out_row;
   int M, N, K, gelu;
-  float* part;   // workspace: gemm_q8_workspace floats
+  float* part;   // workspace: gemm_q8_workspace bytes
 };
-size_t gemm_q8_workspace(int M, int N, int K);
+size_t gemm_q8_workspace(int out_dtype, int M, int N, int K);
 hipError_t gemm_q8(int out_dtype, const GemmQ8Args& a, hipStream_t s);
 
 // ---------------------------------------------------------------- attention over spans

@@ -180,7 +180,7 @@ ff_status ff_rms_norm_q8(const ff_norm_desc* d, const void* x, const void* resid
 }
 
 size_t ff_gemm_q8_workspace_bytes(const ff_gemm_q8_desc* d) {
-  return check_gemm(d, false) ? 0 : gemm_q8_workspace(d->M, d->N, d->K);
+  return check_gemm(d, false) ? 0 : gemm_q8_workspace(d->out_dtype, d->M, d->N, d->K);
 }
 
 ff_status ff_gemm_q8(const ff_gemm_q8_desc* d, const void* a, const float* a_s, const void* w, const float* w_s,
@@ -189,7 +189,7 @@ ff_status ff_gemm_q8(const ff_gemm_q8_desc* d, const void* a, const float* a_s, 
   if (e) return e;
   if (d->M == 0) return ok();
   CHECK(a && a_s && w && w_s && out, FF_E_NULL, "a, a_s, w, w_s or out is NULL");
-  const size_t need = gemm_q8_workspace(d->M, d->N, d->K);
+  const size_t need = gemm_q8_workspace(d->out_dtype, d->M, d->N, d->K);
   CHECK(!need || ws, FF_E_NULL, "ws is NULL");
   CHECK(ws_bytes >= need, FF_E_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
   const void* ps[] = {a, a_s, w, w_s, bias, resid, out, need ? ws : nullptr};

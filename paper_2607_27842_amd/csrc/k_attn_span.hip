@@ -11,6 +11,7 @@ namespace ff {
 
 namespace {
 
+typedef int i32x4_t __attribute__((ext_vector_type(4)));
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kFltMax = 3.402823466e38f;
 constexpr int kKeys = 32;        // keys per wavefront and step of the direct kernels
@@ -91,8 +92,15 @@ __device__ __forceinline__ float score(const AttnSpanArgs& a, const Row& w, floa
 template <bool F32>
 __device__ __forceinline__ float exp_of(float t) { return F32 ? expf(t) : __builtin_amdgcn_exp2f(t); }
 
-// exponents of one bf16 pair / one fp32 value that are all ones: an infinity or a NaN
-__device__ __forceinline__ bool odd_bf16x2(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
+// Largest exponents of bf16 pairs / magnitude of fp32 values so far: all ones tell an infinity or a NaN
+typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
+struct Top {
+  u16x2_t b = {0, 0};
+  uint32_t f = 0u;
+  __device__ __forceinline__ void bf16x2(uint32_t w) { b = __builtin_elementwise_max(b, __builtin_bit_cast(u16x2_t, w & 0x7f807f80u)); }
+  __device__ __forceinline__ void f32(float x) { f = max(f, __float_as_uint(x) & 0x7fffffffu); }
+  __device__ __forceinline__ bool odd() const { return b[0] == 0x7f80u || b[1] == 0x7f80u || f >= 0x7f800000u; }
+};
 __device__ __forceinline__ uint32_t clean_bf16x2(uint32_t w) {
   if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
   if ((w & 0x7f800000u) == 0x7f800000u) w &= 0xffffu;
@@ -123,40 +131,22 @@ __device__ __forceinline__ Place place_of(const AttnSpanArgs& a, int nsplit, int
   return p;
 }
 
-// 16 rows a workgroup; its 4 waves take every fourth step of 32 keys, K straight from memory in
-// operand layout, V (bf16) through the wave's own LDS rows for the transposed reads.  The next
-// step's loads are in flight while this one's scores and products are formed.
+// One wavefront's 16 rows over the keys of [first, end) (first a multiple of 32) in steps of 32, `stride` keys
+// from one step to the next: K straight from memory in operand layout, V (bf16) through the wave's
+// own LDS rows (stg) for the transposed reads.  The next step's loads are in flight while this
+// one's scores and products are formed.  Rows of V that some queries see and others do not may hold
+// an infinity or a NaN, which must not meet a probability of zero: the product is formed without
+// it, and it is added afterwards to the rows that see its key.
+// Result: m (the same in a row's four lanes), l (to be added over them), o.
 template <int DT, int NE>
-__global__ __launch_bounds__(256) void k_attn_dir(AttnSpanArgs a, int nsplit) {
-#ifdef __HIP_DEVICE_COMPILE__   // the host pass needs the launch stub only
+__device__ __forceinline__ void attend16(const AttnSpanArgs& a, const Row& w, const Ranges& rg, const char* qp, const char* kp,
+                                         const char* vp, int first, int end, int stride, char* stg, f32x4_t (&o)[NE], float& m, float& l) {
   constexpr bool F32 = DT == DT_F32;
   constexpr int NC = (NE + 1) / 2;              // bf16: k steps of 32 dims
   constexpr int CPR = NE * 2, NV = kKeys * CPR / 64;   // bf16: 16-byte chunks per V row, per lane
   constexpr int PV = NE * 32 + 16;              // bf16: bytes of a staged V row
-  constexpr int kStage = F32 ? 0 : 4 * kKeys * PV, kMerge = 3 * (NE * 4 + 2) * 64 * 4;
-  __shared__ __attribute__((aligned(1024))) char smem[kStage > kMerge ? kStage : kMerge];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int l16 = lane & 15, g = lane >> 4;
-  const Place P = place_of(a, nsplit, 16);
-  const int R = a.n_q * a.G, d = a.d;
-  const int r = min(P.tile * 16 + l16, R - 1), qi = r / a.G;
-  Row w[1] = {row_of(a, P.b, P.hk, r, qi)};
-  const Ranges rg = ranges_of<1>(w);
-  // this split's part of the rows' keys
-  int first = min(rg.h0, rg.h1), end = max(rg.e0, rg.e1);
-  if (first < end) {
-    first &= ~(4 * kKeys - 1);
-    const int chunk = ((end - first + nsplit - 1) / nsplit + 4 * kKeys - 1) & ~(4 * kKeys - 1);
-    // split * chunk stays below n_k + 64 * 128 < 2^31
-    first += P.split * chunk;
-    end = min(end, first + chunk);
-  } else {
-    first = end = 0;
-  }
-  const size_t es = F32 ? 4 : 2;
-  const char* qp = (const char*)a.q + ((size_t)P.b * a.qb + (size_t)qi * a.qr + (size_t)(P.hk * a.G + r % a.G) * a.qh) * es;
-  const char* kp = (const char*)a.k + ((size_t)P.b * a.kb + (size_t)P.hk * a.kh) * es;
-  const char* vp = (const char*)a.v + ((size_t)P.b * a.vb + (size_t)P.hk * a.vh) * es;
+  constexpr size_t es = F32 ? 4 : 2;
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, d = a.d;
   const f32x4_t z4 = {0.f, 0.f, 0.f, 0.f};
   const u32x4_t zu = {0u, 0u, 0u, 0u};
   constexpr int NQ = F32 ? NE : NC, DQ = F32 ? 16 : 32, EQ = F32 ? 4 : 8;   // operand chunks, dims of each, dims a lane holds
@@ -167,62 +157,75 @@ __global__ __launch_bounds__(256) void k_attn_dir(AttnSpanArgs a, int nsplit) {
     const int e = DQ * c + EQ * g;
     qf[c] = e < d ? *reinterpret_cast<const u32x4_t*>(qp + e * es) : zu;
   }
+  // Keys past the end read the last one (their scores are masked), dims past d the row's first (of K
+  // they count as zeros, of V their products are never stored): no load depends on a lane's mask.
   auto load = [&](int k0) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < 2; ++i) {
+      const char* row = kp + (size_t)min(k0 + 16 * i + l16, end - 1) * a.kr * es;
 #pragma unroll
       for (int c = 0; c < NQ; ++c) {
-        const int k = k0 + 16 * i + l16, e = DQ * c + EQ * g;
-        kf[i][c] = k < end && e < d ? *reinterpret_cast<const u32x4_t*>(kp + ((size_t)k * a.kr + e) * es) : zu;
+        const int e = DQ * c + EQ * g;
+        kf[i][c] = *reinterpret_cast<const u32x4_t*>(row + (c < NQ - 2 || e < d ? e : 0) * es);
       }
+    }
     if constexpr (F32) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
+      for (int j = 0; j < 8; ++j) {
+        const char* row = vp + (size_t)min(k0 + 16 * (j / 4) + 4 * g + j % 4, end - 1) * a.vr * 4;
 #pragma unroll
         for (int c = 0; c < NE; ++c) {
-          const int k = k0 + 16 * (j / 4) + 4 * g + j % 4, e = 16 * c + l16;
-          vv[j][c] = k < end && e < d ? *reinterpret_cast<const float*>(vp + ((size_t)k * a.vr + e) * 4) : 0.f;
+          const int e = 16 * c + l16;
+          vv[j][c] = *reinterpret_cast<const float*>(row + (c < NE - 2 || e < d ? e : 0) * 4);
         }
+      }
     } else {
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
-        const int idx = j * 64 + lane, k = k0 + idx / CPR, e = idx % CPR * 8;
-        vf[j] = k < end && e < d ? *reinterpret_cast<const u32x4_t*>(vp + ((size_t)k * a.vr + e) * 2) : zu;
+        const int idx = j * 64 + lane, e = idx % CPR * 8;
+        vf[j] = *reinterpret_cast<const u32x4_t*>(vp + ((size_t)min(k0 + idx / CPR, end - 1) * a.vr + (e < d ? e : 0)) * 2);
       }
     }
   };
-  f32x4_t o[NE];
+  const bool whole = d == DQ * NQ;
+  auto cut = [&]() __attribute__((always_inline)) {
+    if (whole) return;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int c = NQ > 2 ? NQ - 2 : 0; c < NQ; ++c)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) kf[i][c][x] = DQ * c + EQ * g < d ? kf[i][c][x] : 0u;
+  };
 #pragma unroll
   for (int e = 0; e < NE; ++e) o[e] = z4;
-  float m = -INFINITY, l = 0.f;
-  char* const stg = smem + wave * kKeys * PV;
+  m = -INFINITY;
+  l = 0.f;
   const uint32_t stg0 = (uint32_t)(uintptr_t)((__attribute__((address_space(3))) const void*)stg);
   const uint32_t va = stg0 + (4 * g + (l16 >> 2)) * PV + (l16 & 3) * 8;
   auto next = [&](int k) __attribute__((always_inline)) {   // the next step whose keys some row sees
-    while (k < end && !rg.some(k, kKeys)) k += 4 * kKeys;
+    while (k < end && !rg.some(k, kKeys)) k += stride;
     return k;
   };
-  int k0 = next(first + wave * kKeys);
+  int k0 = next(first);
   if (k0 < end) load(k0);
   while (k0 < end) {
     const bool part = !rg.all(k0, kKeys);
-    // rows that some queries see and others do not: an infinity or a NaN among them must not meet a
-    // probability of zero.  Their products are formed without it, and it is added afterwards to
-    // the rows that see its key.
     bool odd = false;
     if (part) {
+      Top top;
       if constexpr (F32) {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
 #pragma unroll
-          for (int c = 0; c < NE; ++c) odd = odd || odd_f32(vv[j][c]);
+          for (int c = 0; c < NE; ++c) top.f32(vv[j][c]);
       } else {
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) odd = odd || odd_bf16x2(vf[j][e]);
+          for (int e = 0; e < 4; ++e) top.bf16x2(vf[j][e]);
       }
-      odd = __any(odd);
+      odd = __any(top.odd());
       if (odd) {
         if constexpr (F32) {
 #pragma unroll
@@ -245,6 +248,7 @@ __global__ __launch_bounds__(256) void k_attn_dir(AttnSpanArgs a, int nsplit) {
       }
     }
     f32x4_t sc[2] = {z4, z4};
+    cut();
 #pragma unroll
     for (int c = 0; c < NQ; ++c)
 #pragma unroll
@@ -261,8 +265,8 @@ __global__ __launch_bounds__(256) void k_attn_dir(AttnSpanArgs a, int nsplit) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const int k = k0 + 16 * (j / 4) + 4 * g + j % 4;
-      p[j] = score<F32>(a, w[0], sc[j / 4][j % 4], k);
-      if (part && !w[0].sees(k)) p[j] = -INFINITY;
+      p[j] = score<F32>(a, w, sc[j / 4][j % 4], k);
+      if (part && !w.sees(k)) p[j] = -INFINITY;
       x = fmaxf(x, p[j]);
     }
     x = fmaxf(x, __shfl_xor(x, 16, 64));
@@ -291,14 +295,14 @@ __global__ __launch_bounds__(256) void k_attn_dir(AttnSpanArgs a, int nsplit) {
             const f32x4_t y = *reinterpret_cast<const f32x4_t*>(vp + ((size_t)k * a.vr + 16 * c + 4 * g) * 4);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              if (odd_f32(y[e]) && w[0].sees(k)) o[c][e] += y[e];
+              if (odd_f32(y[e]) && w.sees(k)) o[c][e] += y[e];
           }
       }
-      k0 = next(k0 + 4 * kKeys);
+      k0 = next(k0 + stride);
       if (k0 < end) load(k0);
     } else {
       const int kk = k0;
-      k0 = next(k0 + 4 * kKeys);
+      k0 = next(k0 + stride);
       if (k0 < end) load(k0);
       const u32x4_t pw = {pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])};
       u32x2_t vt[NE][2];
@@ -324,12 +328,47 @@ __global__ __launch_bounds__(256) void k_attn_dir(AttnSpanArgs a, int nsplit) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const float f = __uint_as_float(e & 1 ? y[e / 2] & 0xffff0000u : y[e / 2] << 16);
-              if (odd_f32(f) && w[0].sees(k)) o[c][e] += f;
+              if (odd_f32(f) && w.sees(k)) o[c][e] += f;
             }
           }
       }
     }
   }
+}
+
+// 16 rows a workgroup, whose 4 waves take every fourth step of 32 keys.
+template <int DT, int NE>
+__global__ __launch_bounds__(256) void k_attn_dir(AttnSpanArgs a, int nsplit) {
+#ifdef __HIP_DEVICE_COMPILE__   // the host pass needs the launch stub only
+  constexpr bool F32 = DT == DT_F32;
+  constexpr int PV = NE * 32 + 16;              // bf16: bytes of a staged V row
+  constexpr int kStage = F32 ? 0 : 4 * kKeys * PV, kMerge = 3 * (NE * 4 + 2) * 64 * 4;
+  __shared__ __attribute__((aligned(1024))) char smem[kStage > kMerge ? kStage : kMerge];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l16 = lane & 15, g = lane >> 4;
+  const Place P = place_of(a, nsplit, 16);
+  const int R = a.n_q * a.G, d = a.d;
+  const int r = min(P.tile * 16 + l16, R - 1), qi = r / a.G;
+  Row w[1] = {row_of(a, P.b, P.hk, r, qi)};
+  const Ranges rg = ranges_of<1>(w);
+  // this split's part of the rows' keys
+  int first = min(rg.h0, rg.h1), end = max(rg.e0, rg.e1);
+  if (first < end) {
+    first &= ~(4 * kKeys - 1);
+    const int chunk = ((end - first + nsplit - 1) / nsplit + 4 * kKeys - 1) & ~(4 * kKeys - 1);
+    // split * chunk stays below n_k + 64 * 128 < 2^31
+    first += P.split * chunk;
+    end = min(end, first + chunk);
+  } else {
+    first = end = 0;
+  }
+  const size_t es = F32 ? 4 : 2;
+  const char* qp = (const char*)a.q + ((size_t)P.b * a.qb + (size_t)qi * a.qr + (size_t)(P.hk * a.G + r % a.G) * a.qh) * es;
+  const char* kp = (const char*)a.k + ((size_t)P.b * a.kb + (size_t)P.hk * a.kh) * es;
+  const char* vp = (const char*)a.v + ((size_t)P.b * a.vb + (size_t)P.hk * a.vh) * es;
+  f32x4_t o[NE];
+  float m, l;
+  attend16<DT, NE>(a, w[0], rg, qp, kp, vp, first + wave * kKeys, end, 4 * kKeys, smem + wave * kKeys * PV, o, m, l);
   // the waves' (m, l, O) merge in wave order; l is per lane, m common to a row's four lanes
   float (*xch)[NE * 4 + 2][64] = reinterpret_cast<float (*)[NE * 4 + 2][64]>(smem);
   __syncthreads();   // every wave is done with its staged rows
@@ -405,6 +444,434 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnSpanArgs a, int nsplit, i
   }
 }
 
+// ---------------------------------------------------------------- bf16, many rows: two wave groups in turn
+// 8 waves of 16 QT rows in two groups of four (one wave of each per SIMD), 64-key tiles of K and V in
+// rings of four, as in the blocks' own attention (k_attn_pp, where the slots, the layouts and what
+// bounds them stand).  Per tile a wave has a softmax slot (the tile's probabilities, and the DMA of
+// the tiles three and two ahead) and an MFMA slot (the next tile's scores, then this tile's P V),
+// each ended by a barrier; the second group runs one slot behind.
+// A workgroup walks the tiles that its rows' spans meet.  Per tile a wave knows whether all its rows
+// see all keys (no mask), some (each score is tested against its row's spans), or none (zero
+// probabilities at once).
+// MOD: capped or biased scores, formed in log2 units before the softmax.
+// (two workgroups share a CU where a K or V row takes 128 bytes of LDS: at most 128 VGPRs)
+template <int RWB, int NC, int NE, int QT, bool MOD>
+__global__ __launch_bounds__(512, RWB == 128 ? 4 : 2) void k_attn_span_pp(AttnSpanArgs a) {
+#ifdef __HIP_DEVICE_COMPILE__   // the host pass needs the launch stub only
+  constexpr int KB = 64, NB = 4;                 // keys per tile, ring depth
+  constexpr int TB = KB * RWB;                   // bytes of a K (or V) tile
+  constexpr int DPW = RWB / 128;                 // DMA instructions per wave, tile and operand
+  constexpr int CPR = RWB / 16;                  // 16-byte chunks per LDS row
+  static_assert(NC * 64 <= RWB && NE * 32 <= RWB, "head dim tiles fit the LDS row");
+  constexpr int LDO = NE * 16 + 8;               // staged output row pitch (elements)
+  constexpr int kMain = 2 * NB * TB, kOut = 8 * 16 * QT * LDO * 2;
+  constexpr float kPLim = 256.0f;                // as in k_attn_pp: what raises a row's running maximum
+  constexpr int kRows = kMain > kOut ? kMain : kOut;   // behind it, the rows' spans (read where a tile needs a mask)
+  __shared__ __attribute__((aligned(1024))) char smem[kRows + 128 * QT * 16];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l16 = lane & 15, g = lane >> 4;
+  const int R = a.n_q * a.G, d = a.d;
+  int qb, hk, b;
+  {
+    // an XCD gets neighbouring places; the last rows, which see the most keys under a causal mask, first
+    const int nqb = (R + 128 * QT - 1) / (128 * QT), n = gridDim.x, id = blockIdx.x;
+    const int full = n / 8 * 8;
+    const int t = id < full ? (id % 8) * (full / 8) + id / 8 : id;
+    qb = __builtin_amdgcn_readfirstlane(nqb - 1 - t % nqb);
+    hk = __builtin_amdgcn_readfirstlane((t / nqb) % a.H_kv);
+    b = __builtin_amdgcn_readfirstlane(t / (nqb * a.H_kv));
+  }
+  const int q0 = qb * 128 * QT + wave * 16 * QT;
+  Row rows[QT];
+  bf16x8_t qf[QT][NC];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    const int r = min(q0 + 16 * t + l16, R - 1), i = r / a.G;
+    rows[t] = row_of(a, b, hk, r, i);
+    const uint16_t* qp = (const uint16_t*)a.q + (size_t)b * a.qb + (size_t)i * a.qr + (size_t)(hk * a.G + r % a.G) * a.qh;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const int e = 32 * c + 8 * g;
+      u32x4_t v = {0u, 0u, 0u, 0u};
+      if (e < d) v = *reinterpret_cast<const u32x4_t*>(qp + e);
+      qf[t][c] = __builtin_bit_cast(bf16x8_t, v);
+    }
+  }
+  const Ranges rg = ranges_of<QT>(rows);
+  int pos[QT];
+  const float* bias[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    pos[t] = rows[t].pos;
+    bias[t] = rows[t].bias;
+    if (g == 0) *reinterpret_cast<i32x4_t*>(smem + kRows + (wave * 16 * QT + 16 * t + l16) * 16) = i32x4_t{rows[t].lo0, rows[t].n0, rows[t].lo1, rows[t].n1};
+  }
+  // the workgroup's tiles: those of the first hull, then those of the second beyond it, ascending
+  int t0, n0, t1, nt;
+  {
+    int* const x = reinterpret_cast<int*>(smem);
+    if (lane == 0) {
+      x[wave * 4] = rg.h0; x[wave * 4 + 1] = rg.e0; x[wave * 4 + 2] = rg.h1; x[wave * 4 + 3] = rg.e1;
+    }
+    __syncthreads();
+    int h0 = 0x7fffffff, e0 = 0, h1 = 0x7fffffff, e1 = 0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+      h0 = min(h0, x[w * 4]); e0 = max(e0, x[w * 4 + 1]); h1 = min(h1, x[w * 4 + 2]); e1 = max(e1, x[w * 4 + 3]);
+    }
+    __syncthreads();
+    int a0 = h0 / KB, b0 = (e0 + KB - 1) / KB, a1 = h1 / KB, b1 = (e1 + KB - 1) / KB;
+    if (e0 <= 0) a0 = b0 = 0;
+    if (e1 <= 0) a1 = b1 = 0;
+    if (b0 == a0) { a0 = a1; b0 = b1; a1 = b1 = 0; }                        // one range, if any, comes first
+    if (b1 > a1 && a1 < a0) { const int p = a0, q = b0; a0 = a1; b0 = b1; a1 = p; b1 = q; }
+    if (b1 > a1 && a1 <= b0) { b0 = max(b0, b1); a1 = b1 = 0; }             // meeting ranges are one
+    t0 = __builtin_amdgcn_readfirstlane(a0);
+    n0 = __builtin_amdgcn_readfirstlane(b0 - a0);
+    t1 = __builtin_amdgcn_readfirstlane(a1);
+    nt = __builtin_amdgcn_readfirstlane(b0 - a0 + b1 - a1);
+  }
+  auto tile_of = [&](int j) __attribute__((always_inline)) { return j < n0 ? t0 + j : t1 + j - n0; };
+  const char* const kp = (const char*)a.k + ((size_t)b * a.kb + (size_t)hk * a.kh) * 2;
+  const char* const vp = (const char*)a.v + ((size_t)b * a.vb + (size_t)hk * a.vh) * 2;
+  // the rows of an LDS tile are rotated by f(row) among their 16-byte chunks, so that both the
+  // K reads (16 rows, one chunk) and the transposed V reads (8 rows, one chunk pair) of a
+  // pass spread over all banks
+  auto swz = [](int row) {
+    const int hi = (row >> 3) & 1;
+    return (CPR == 16 ? ((row & 7) ^ (hi << 2)) : (((row >> 1) & 3) ^ (hi << 1))) << 1 | hi;
+  };
+  uint32_t vok[DPW], vov[DPW];   // this lane's byte offsets within a tile; past d: out of range (zeros)
+#pragma unroll
+  for (int j = 0; j < DPW; ++j) {
+    const int idx = (wave * DPW + j) * 64 + lane, row = idx / CPR, e = ((idx % CPR) ^ swz(row)) * 8;
+    vok[j] = e < d ? (uint32_t)row * (uint32_t)a.kr * 2u + (uint32_t)e * 2u : 0x80000000u;
+    vov[j] = e < d ? (uint32_t)row * (uint32_t)a.vr * 2u + (uint32_t)e * 2u : 0x80000000u;
+  }
+  // DMA of tile number *j of the walk into ring slot *slot.  The tile's resource ends with the last key's
+  // last element, so that keys past it, and tiles past the walk, load as zeros (or, with a stride
+  // below d, as elements of the last keys: their probabilities are zero)
+  auto load = [&](const char* base, int64_t ld, const uint32_t (&vo)[DPW], int off, int* j, int* slot) __attribute__((always_inline)) {
+    const int tile = tile_of(*j), left = *j < nt ? min(a.n_k - tile * KB, KB) : 0;
+    const uint32_t num = left > 0 ? (uint32_t)((left - 1) * ld + d) * 2u : 0u;
+    __amdgpu_buffer_rsrc_t rs =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base) + (left > 0 ? (size_t)tile * KB * ld * 2 : 0), 0, num, 0x00020000);
+#pragma unroll
+    for (int i = 0; i < DPW; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, FF_AS3(smem + off + *slot + (wave * DPW + i) * 1024), 16, vo[i], 0, 0, 0);
+    ++*j;
+    *slot = *slot == (NB - 1) * TB ? 0 : *slot + TB;
+  };
+  int ktile = 0, vtile = 0, kslot = 0, vslot = 0;
+  auto load_k = [&]() __attribute__((always_inline)) { load(kp, a.kr, vok, 0, &ktile, &kslot); };
+  auto load_v = [&]() __attribute__((always_inline)) { load(vp, a.vr, vov, NB * TB, &vtile, &vslot); };
+  // fragment addresses within a tile (k step c and output tile e enter by xor)
+  const uint32_t lds0 = (uint32_t)(uintptr_t)((__attribute__((address_space(3))) const void*)smem);
+  const uint32_t ka = lds0 + l16 * RWB + ((g ^ swz(l16)) * 16);
+  const int vr = 4 * g + (l16 >> 2);
+  const uint32_t va = lds0 + NB * TB + vr * RWB + ((((l16 & 3) >> 1) ^ swz(vr)) * 16) + (l16 & 1) * 8;
+  f32x4_t o[NE][QT], sc[4][QT];
+#pragma unroll
+  for (int e = 0; e < NE; ++e)
+#pragma unroll
+    for (int t = 0; t < QT; ++t) o[e][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  float m[QT], l[QT], lim[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) { m[t] = -INFINITY; l[t] = 0.f; lim[t] = -1.f; }
+  const float sl2 = MOD ? 1.f : a.scale * kLog2e;
+  bf16x8_t pb[2][QT];
+  int ks = 0, vs = 0;            // ring slots being read
+  // The MFMA slot of a tile is a chain of units of two A fragments and 2 QT MFMAs: first
+  // the 2 NC units of the next tile's scores (K fragments), then the NE units of this tile's
+  // PV product (V^T fragments, each two transposed reads).  A unit's reads are issued UD
+  // units ahead.
+  constexpr int UK = 2 * NC, UV = NE, UD = 3;
+  bf16x8_t kf[UD + 1][2];
+  u32x2_t vf[UD + 1][2][2] = {};
+  uint32_t ka_ = ka, va_ = va;
+  auto rd = [&](auto Uc) __attribute__((always_inline)) {
+    constexpr int U = decltype(Uc)::value;
+    if constexpr (U < UK) {
+      constexpr int c = U / 2, i0 = U % 2 * 2;
+      const uint32_t ad = ka_ ^ (c * 64);
+      kf[U % (UD + 1)][0] = lds_rd128_at<i0 * 16 * RWB>(ad);
+      kf[U % (UD + 1)][1] = lds_rd128_at<(i0 + 1) * 16 * RWB>(ad);
+    } else if constexpr (U < UK + UV) {
+      constexpr int f = 2 * (U - UK);
+      const uint32_t a0 = va_ ^ (f % NE * 32), a1 = va_ ^ ((f + 1) % NE * 32);
+      vf[U % (UD + 1)][0][0] = lds_rd64_tr(a0, f / NE * 32 * RWB);
+      vf[U % (UD + 1)][0][1] = lds_rd64_tr(a0, f / NE * 32 * RWB + 16 * RWB);
+      vf[U % (UD + 1)][1][0] = lds_rd64_tr(a1, (f + 1) / NE * 32 * RWB);
+      vf[U % (UD + 1)][1][1] = lds_rd64_tr(a1, (f + 1) / NE * 32 * RWB + 16 * RWB);
+    }
+  };
+  auto unit = [&](auto Uc) __attribute__((always_inline)) {
+    constexpr int U = decltype(Uc)::value;
+    rd(Int<U + UD>{});
+    constexpr int later = (U + 1 < UK + UV ? (U + 1 < UK ? 2 : 4) : 0) + (U + 2 < UK + UV ? (U + 2 < UK ? 2 : 4) : 0) +
+                          (U + 3 < UK + UV ? (U + 3 < UK ? 2 : 4) : 0);
+    asm volatile("s_waitcnt lgkmcnt(%0)" ::"n"(later) : "memory");
+    constexpr int buf = U % (UD + 1);
+    if constexpr (U < UK) {
+      FF_TIE(kf[buf][0]); FF_TIE(kf[buf][1]);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+          constexpr int c = U / 2, i0 = U % 2 * 2;
+          sc[i0 + i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[buf][i], qf[t][c], c == 0 ? f32x4_t{0.f, 0.f, 0.f, 0.f} : sc[i0 + i][t], 0, 0, 0);
+        }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) { FF_TIE(vf[buf][i][0]); FF_TIE(vf[buf][i][1]); }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        constexpr int f0 = 2 * (U - UK);
+        const int s = (f0 + i) / NE, e = (f0 + i) % NE;
+        const u32x4_t w = {vf[buf][i][0][0], vf[buf][i][0][1], vf[buf][i][1][0], vf[buf][i][1][1]};
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+          o[e][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, w), pb[s][t], o[e][t], 0, 0, 0);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // the V reads that run ahead of a chain of scores alone are used nowhere, but hold their
+  // registers until they are in
+  auto drain = [&]() __attribute__((always_inline)) {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < (UD + 1) * 4; ++i) FF_TIE(vf[i / 4][i / 2 % 2][i % 2]);
+  };
+#define FF_BAR() asm volatile("s_barrier" ::: "memory")
+  auto spans_at = [&](int t) __attribute__((always_inline)) {
+    i32x4_t w;
+    asm volatile("ds_read_b128 %0, %1 offset:%2\n\ts_waitcnt lgkmcnt(0)" : "=v"(w) : "v"(lds0 + kRows + (wave * 16 * QT + l16) * 16), "i"(t * 256) : "memory");
+    return w;
+  };
+  auto sees = [](i32x4_t w, int k) __attribute__((always_inline)) {
+    return (unsigned)(k - w[0]) < (unsigned)w[1] || (unsigned)(k - w[2]) < (unsigned)w[3];
+  };
+  // a row's bias beyond the table's reach, on either side (log2 units)
+  float below[MOD ? QT : 1], above[MOD ? QT : 1];
+  if constexpr (MOD) {
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      below[t] = a.bias_kind == BIAS_TABLE ? bias[t][-a.reach] : a.bias_kind == BIAS_SLOPE ? bias[t][0] : 0.f;
+      above[t] = a.bias_kind == BIAS_TABLE ? bias[t][a.reach] : 0.f;
+    }
+  }
+  // sc -> scores in log2 units
+  auto modify = [&](int k0) __attribute__((always_inline)) {
+    if (a.cap > 0.f) {
+      const float c1 = 2.f * kLog2e * a.scale / a.cap, c2 = a.cap;
+#pragma unroll
+      for (int t = 0; t < QT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int v = 0; v < 4; ++v)
+            sc[i][t][v] = fmaf(-2.f * c2, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(c1 * sc[i][t][v])), c2);
+    } else {
+#pragma unroll
+      for (int t = 0; t < QT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sc[i][t] *= a.scale;
+    }
+    if (a.bias_kind == BIAS_SLOPE) {
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        const float at = (float)(k0 + 4 * g - pos[t]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) sc[i][t][v] = fmaf(-below[t], fabsf(at + (float)(16 * i + v)), sc[i][t][v]);
+      }
+    } else if (a.bias_kind == BIAS_TABLE) {
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        const int at = k0 - pos[t];   // the tile's first distance
+        const bool lo = __all(at + KB - 1 <= -a.reach), hi = __all(at >= a.reach);
+        if (lo || hi) {
+          const float c = lo ? below[t] : above[t];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sc[i][t] += c;
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) sc[i][t][v] += bias[t][min(max(at + 16 * i + 4 * g + v, -a.reach), a.reach)];
+        }
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < QT; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {   // a finite score stays finite
+          const float x = sc[i][t][v], y = x * kLog2e;
+          sc[i][t][v] = fabsf(x) <= kFltMax ? fminf(fmaxf(y, -kFltMax), kFltMax) : y;
+        }
+  };
+  // sc -> probabilities pb (complete when it returns: nothing of it moves past the barrier)
+  auto softmax = [&](int k0, bool some, bool part) __attribute__((always_inline)) {
+    if (!some) {
+#pragma unroll
+      for (int t = 0; t < QT; ++t) pb[0][t] = pb[1][t] = __builtin_bit_cast(bf16x8_t, u32x4_t{0u, 0u, 0u, 0u});
+    } else {
+      if constexpr (MOD) modify(k0);
+      if (part) {
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+          const i32x4_t w = spans_at(t);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+              sc[i][t][v] = sees(w, k0 + 16 * i + 4 * g + v) ? sc[i][t][v] : -INFINITY;
+        }
+      }
+      // probabilities against the running maxima m (log2 units), raised only where a lane's 16
+      // probabilities of a row add up to more than kPLim or are not all numbers
+      float p[QT][16], ps[QT];
+      bool up = false;
+      auto probs = [&](int t) __attribute__((always_inline)) {
+        const float mo = m[t] == -INFINITY ? 0.f : m[t];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) p[t][i] = __builtin_amdgcn_exp2f(MOD ? sc[i / 4][t][i % 4] - mo : fmaf(sc[i / 4][t][i % 4], sl2, -mo));
+        float s4[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s4[i] = (p[t][4 * i] + p[t][4 * i + 1]) + (p[t][4 * i + 2] + p[t][4 * i + 3]);
+        ps[t] = (s4[0] + s4[1]) + (s4[2] + s4[3]);
+      };
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        probs(t);
+        up = up || !(ps[t] <= lim[t]);
+      }
+      if (__any(up)) {
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+          float x = -INFINITY;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) x = fmaxf(x, sc[i / 4][t][i % 4]);
+          x = fmaxf(x, __shfl_xor(x, 16, 64));         // the four lanes of a row together
+          x = fmaxf(x, __shfl_xor(x, 32, 64)) * sl2;   // scale > 0: max commutes with it
+          const float mn = fmaxf(m[t], ceilf(x));      // whole: the rescale is by a power of two, exact
+          const float al = mn == m[t] ? 1.f : __builtin_amdgcn_exp2f(m[t] - mn);   // exp2(-inf) = 0
+          m[t] = mn;
+          lim[t] = mn == -INFINITY ? -1.f : kPLim;     // -1: the next tile comes here too
+          l[t] *= al;
+#pragma unroll
+          for (int e = 0; e < NE; ++e) o[e][t] *= al;
+          probs(t);
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        l[t] += ps[t];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const float* q = &p[t][8 * s];
+          const u32x4_t w = {pack_bf16x2(q[0], q[1]), pack_bf16x2(q[2], q[3]), pack_bf16x2(q[4], q[5]), pack_bf16x2(q[6], q[7])};
+          pb[s][t] = __builtin_bit_cast(bf16x8_t, w);
+        }
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < QT; ++t) { FF_TIE(pb[0][t]); FF_TIE(pb[1][t]); FF_TIE(l[t]); }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  bool mixed = false;   // some tile held keys that a row does not see
+  if (nt > 0) {
+    load_k();
+    load_k(); load_v();
+    load_k(); load_v();
+    wait_vm<2 * DPW>();
+    FF_BAR();
+    static_for<0, UD>(rd);
+    static_for<0, UK>(unit);   // the first tile's scores
+    drain();
+    ks = TB;
+    if (wave >= 4) FF_BAR();   // the second group runs one slot behind
+    for (int j = 0; j < nt; ++j) {
+      const int k0 = tile_of(j) * KB;
+      const bool some = rg.some(k0, KB), part = some && !rg.all(k0, KB);
+      mixed = mixed || part || !some;
+      load_k();
+      load_v();
+      __builtin_amdgcn_sched_barrier(0);
+      softmax(k0, some, part);
+      ka_ = ka + ks;
+      va_ = va + vs;
+      static_for<0, UD>(rd);
+      wait_vm<2 * DPW>();
+      FF_BAR();
+      __builtin_amdgcn_s_setprio(1);
+      static_for<0, UK + UV>(unit);
+      __builtin_amdgcn_s_setprio(0);
+      FF_BAR();
+      ks = ks == (NB - 1) * TB ? 0 : ks + TB;
+      vs = vs == (NB - 1) * TB ? 0 : vs + TB;
+    }
+    wait_vm<0>();
+    if (wave < 4) FF_BAR();
+    FF_BAR();   // the DMA of every wave has ended, before the staging below
+  }
+#undef FF_BAR
+  // An infinity or a NaN in a row of V that a query does not see has met its probability of zero: such
+  // results are not numbers, and the wavefront's rows are formed again without it (attend16).
+  // Results that are not numbers by right come here too.
+  if (mixed) {
+    Top top;
+#pragma unroll
+    for (int e = 0; e < NE; ++e)
+#pragma unroll
+      for (int t = 0; t < QT; ++t)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) top.f32(o[e][t][v]);
+    if (__builtin_expect(__any(top.odd()), 0)) {
+      static_assert(kKeys * (NE * 32 + 16) * 8 <= kRows, "a wavefront's staged V rows");
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        const int r = min(q0 + 16 * t + l16, R - 1), i = r / a.G;
+        const Row w[1] = {row_of(a, b, hk, r, i)};
+        const Ranges rt = ranges_of<1>(w);
+        const char* qp = (const char*)((const uint16_t*)a.q + (size_t)b * a.qb + (size_t)i * a.qr + (size_t)(hk * a.G + r % a.G) * a.qh);
+        const int end = max(rt.e0, rt.e1);
+        f32x4_t x[NE];
+        attend16<DT_BF16, NE>(a, w[0], rt, qp, kp, vp, end > 0 ? min(rt.h0, rt.h1) & ~(kKeys - 1) : 0, end, kKeys,
+                              smem + wave * kKeys * (NE * 32 + 16), x, m[t], l[t]);
+#pragma unroll
+        for (int e = 0; e < NE; ++e) o[e][t] = x[e];
+      }
+    }
+  }
+  // o[e][t][v] = O[row q0 + 16 t + l16][16 e + 4 g + v], staged through the wave's own LDS
+  // region and stored as 16-byte row pieces
+  uint16_t* stg = reinterpret_cast<uint16_t*>(smem) + wave * 16 * QT * LDO;
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    float s = l[t] + __shfl_xor(l[t], 16, 64);
+    s += __shfl_xor(s, 32, 64);
+    const float inv = s == 0.f ? 0.f : 1.0f / s;   // no key seen: zeros
+#pragma unroll
+    for (int e = 0; e < NE; ++e)
+      *reinterpret_cast<u32x2_t*>(stg + (16 * t + l16) * LDO + 16 * e + 4 * g) =
+          u32x2_t{pack_bf16x2(o[e][t][0] * inv, o[e][t][1] * inv), pack_bf16x2(o[e][t][2] * inv, o[e][t][3] * inv)};
+  }
+  uint16_t* out = reinterpret_cast<uint16_t*>(a.out) + (size_t)b * a.ob;
+  const int ppr = d / 8;
+  for (int idx = lane; idx < 16 * QT * ppr; idx += 64) {
+    const int row = idx / ppr, pc = idx - row * ppr, r = q0 + row;
+    if (r < R)
+      *reinterpret_cast<u32x4_t*>(out + (size_t)(r / a.G) * a.orow + (size_t)(hk * a.G + r % a.G) * a.oh + pc * 8) =
+          *reinterpret_cast<const u32x4_t*>(stg + row * LDO + pc * 8);
+  }
+#endif
+}
+
 int splits(long tiles, int n_k) {
   // four workgroups a CU, each with 256 keys or more
   const long by_grid = 1024 / (tiles > 0 ? tiles : 1), by_keys = n_k / 256;
@@ -412,6 +879,31 @@ int splits(long tiles, int n_k) {
   return (int)(n < 1 ? 1 : n > kMaxSplit ? kMaxSplit : n);
 }
 int pieces(int d) { return d <= 32 ? 2 : d <= 48 ? 3 : d <= 64 ? 4 : d <= 80 ? 5 : d <= 96 ? 6 : 8; }
+template <bool MOD>
+hipError_t launch_pp_mod(const AttnSpanArgs& a, hipStream_t s) {
+  // 16 rows a wave for d <= 64 (two workgroups then share a CU); above, 16 or 32, as k_attn_pp
+  const long hb = (long)a.H_kv * a.B, R = (long)a.n_q * a.G, w2 = (R + 255) / 256 * hb, w1 = (R + 127) / 128 * hb;
+  // (32 with capped or biased scores does not fit the registers)
+  const bool two = !MOD && a.d > 64 && (double)((w2 + 255) / 256) <= 0.63 * ((w1 + 255) / 256);
+  const long nwg = two ? w2 : w1;
+  if (nwg > 0x7fffffffL) return hipErrorInvalidValue;
+#define FF_ATTN(RWB, NC, NE)                                                                                       \
+  do {                                                                                                             \
+    if constexpr (RWB > 128 && !MOD)                                                                               \
+      if (two) { FF_LAUNCH((k_attn_span_pp<RWB, NC, NE, 2, MOD>), (unsigned)nwg, 512, 0, s, a); break; }           \
+    FF_LAUNCH((k_attn_span_pp<RWB, NC, NE, 1, MOD>), (unsigned)nwg, 512, 0, s, a);                                 \
+  } while (0)
+  if (a.d <= 48) FF_ATTN(128, 2, 3);
+  else if (a.d <= 64) FF_ATTN(128, 2, 4);
+  else if (a.d <= 80) FF_ATTN(256, 3, 5);
+  else if (a.d <= 96) FF_ATTN(256, 3, 6);
+  else FF_ATTN(256, 4, 8);
+#undef FF_ATTN
+  return hipGetLastError();
+}
+hipError_t launch_pp(const AttnSpanArgs& a, hipStream_t s) {
+  return a.cap > 0.f || a.bias_kind != BIAS_NONE ? launch_pp_mod<true>(a, s) : launch_pp_mod<false>(a, s);
+}
 long tiles16(int B, int H_kv, int G, int n_q) { return (long)B * H_kv * (((long)n_q * G + 15) / 16); }
 
 }  // namespace
@@ -425,6 +917,7 @@ size_t attention_span_workspace(int, int B, int H_kv, int G, int d, int n_q, int
 hipError_t attention_span(int dtype, const AttnSpanArgs& a, hipStream_t s) {
   if (a.n_q <= 0) return hipSuccess;
   const long t = tiles16(a.B, a.H_kv, a.G, a.n_q);
+  if (dtype == DT_BF16 && (long)a.n_q * a.G > 64) return launch_pp(a, s);
   const int n = splits(t, a.n_k), ne = pieces(a.d);
   if (t * n > 0x7fffffffL) return hipErrorInvalidValue;
 #define FF_DIR(DT, NE) FF_LAUNCH((k_attn_dir<DT, NE>), (unsigned)(t * n), 256, 0, s, a, n)

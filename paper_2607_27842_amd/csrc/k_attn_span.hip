@@ -17,14 +17,19 @@ constexpr float kFltMax = 3.402823466e38f;
 constexpr int kKeys = 32;        // keys per wavefront and step of the direct kernels
 constexpr int kMaxSplit = 64;
 
+// r / G and r % G of a row r < 2^30: mul = ceil(2^(31 + shift) / G) with 2^shift >= G is exact
+__device__ __forceinline__ int query_of(const AttnSpanArgs& a, int r) { return (int)(((uint64_t)(uint32_t)r * a.gmul) >> (31 + a.gshift)); }
+
 // What a lane keeps of its row.  Rows past the last repeat it (never stored).
 struct Row {
   int lo0, n0, lo1, n1;   // the spans' first keys and lengths
   int pos;                // where the query stands among the keys
   const float* bias;      // its head's slope, or the middle of its table
+  __device__ __forceinline__ bool none() const { return n0 == 0 && n1 == 0; }
   __device__ __forceinline__ bool sees(int k) const { return (unsigned)(k - lo0) < (unsigned)n0 || (unsigned)(k - lo1) < (unsigned)n1; }
 };
-__device__ __forceinline__ Row row_of(const AttnSpanArgs& a, int b, int hk, int r, int i) {
+// h: its head within the key head's
+__device__ __forceinline__ Row row_of(const AttnSpanArgs& a, int b, int hk, int h, int i) {
   Row w{0, a.n_k, 0, 0, i, nullptr};
   if (a.n_spans) {
     const int32_t* s = a.spans + (size_t)b * a.span_batch + (size_t)i * a.n_spans * 2;
@@ -37,7 +42,7 @@ __device__ __forceinline__ Row row_of(const AttnSpanArgs& a, int b, int hk, int 
   }
   if (a.bias_kind != BIAS_NONE) {
     if (a.pos) w.pos += min(max(a.pos[b], -(1 << 30)), 1 << 30);   // j - p_i stays an int32
-    const int h = hk * a.G + r % a.G;
+    h += hk * a.G;
     w.bias = a.bias + (a.bias_kind == BIAS_TABLE ? (size_t)h * (2 * a.reach + 1) + a.reach : (size_t)h);
   }
   return w;
@@ -66,10 +71,14 @@ __device__ __forceinline__ Ranges ranges_of(const Row (&w)[QT]) {
   for (int t = 0; t < QT; ++t) {
     if (w[t].n0) { h0 = min(h0, w[t].lo0); e0 = max(e0, w[t].lo0 + w[t].n0); }
     if (w[t].n1) { h1 = min(h1, w[t].lo1); e1 = max(e1, w[t].lo1 + w[t].n1); }
+    if (w[t].none()) continue;   // gets zeros whatever is formed for it: its wavefront needs no mask
     c0 = max(c0, w[t].lo0); d0 = min(d0, w[t].lo0 + w[t].n0);
     c1 = max(c1, w[t].lo1); d1 = min(d1, w[t].lo1 + w[t].n1);
   }
-  return Ranges{min16(h0), -min16(-e0), min16(h1), -min16(-e1), -min16(-c0), min16(d0), -min16(-c1), min16(d1)};
+  Ranges r{min16(h0), -min16(-e0), min16(h1), -min16(-e1), -min16(-c0), min16(d0), -min16(-c1), min16(d1)};
+  r.d0 = min(r.d0, r.e0);   // (no rows at all: an empty core)
+  r.d1 = min(r.d1, r.e1);
+  return r;
 }
 
 // The score of key k from the product x = q . k: natural units in fp32, log2 units in bf16 (where its
@@ -334,6 +343,12 @@ __device__ __forceinline__ void attend16(const AttnSpanArgs& a, const Row& w, co
       }
     }
   }
+  if (w.none()) {
+    m = -INFINITY;
+    l = 0.f;
+#pragma unroll
+    for (int e = 0; e < NE; ++e) o[e] = z4;
+  }
 }
 
 // 16 rows a workgroup, whose 4 waves take every fourth step of 32 keys.
@@ -348,8 +363,8 @@ __global__ __launch_bounds__(256) void k_attn_dir(AttnSpanArgs a, int nsplit) {
   const int l16 = lane & 15, g = lane >> 4;
   const Place P = place_of(a, nsplit, 16);
   const int R = a.n_q * a.G, d = a.d;
-  const int r = min(P.tile * 16 + l16, R - 1), qi = r / a.G;
-  Row w[1] = {row_of(a, P.b, P.hk, r, qi)};
+  const int r = min(P.tile * 16 + l16, R - 1), qi = query_of(a, r), qh = r - qi * a.G;
+  Row w[1] = {row_of(a, P.b, P.hk, qh, qi)};
   const Ranges rg = ranges_of<1>(w);
   // this split's part of the rows' keys
   int first = min(rg.h0, rg.h1), end = max(rg.e0, rg.e1);
@@ -363,7 +378,7 @@ __global__ __launch_bounds__(256) void k_attn_dir(AttnSpanArgs a, int nsplit) {
     first = end = 0;
   }
   const size_t es = F32 ? 4 : 2;
-  const char* qp = (const char*)a.q + ((size_t)P.b * a.qb + (size_t)qi * a.qr + (size_t)(P.hk * a.G + r % a.G) * a.qh) * es;
+  const char* qp = (const char*)a.q + ((size_t)P.b * a.qb + (size_t)qi * a.qr + (size_t)(P.hk * a.G + qh) * a.qh) * es;
   const char* kp = (const char*)a.k + ((size_t)P.b * a.kb + (size_t)P.hk * a.kh) * es;
   const char* vp = (const char*)a.v + ((size_t)P.b * a.vb + (size_t)P.hk * a.vh) * es;
   f32x4_t o[NE];
@@ -408,7 +423,7 @@ __global__ __launch_bounds__(256) void k_attn_dir(AttnSpanArgs a, int nsplit) {
   }
   if (P.tile * 16 + l16 >= R) return;
   const float inv = s == 0.f ? 0.f : 1.f / s;   // no key seen: zeros
-  const size_t oo = (size_t)P.b * a.ob + (size_t)qi * a.orow + (size_t)(P.hk * a.G + r % a.G) * a.oh;
+  const size_t oo = (size_t)P.b * a.ob + (size_t)qi * a.orow + (size_t)(P.hk * a.G + qh) * a.oh;
 #pragma unroll
   for (int c = 0; c < NE; ++c)
     if (16 * c + 4 * g < d) store_o4<DT>(a.out, oo + 16 * c + 4 * g, o[c] * inv);
@@ -436,7 +451,8 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnSpanArgs a, int nsplit, i
   const float f = exp_of<DT == DT_F32>(ms - (m == -INFINITY ? 0.f : m));
   const float l = wave_sum(ls * f);
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  const size_t oo = (size_t)b * a.ob + (size_t)(r / a.G) * a.orow + (size_t)(hk * a.G + r % a.G) * a.oh;
+  const int qi = query_of(a, r);
+  const size_t oo = (size_t)b * a.ob + (size_t)qi * a.orow + (size_t)(hk * a.G + r - qi * a.G) * a.oh;
   for (int e = lane; e < a.d; e += 64) {
     float x = 0.f;
     for (int s = 0; s < nsplit; ++s) x += pt[(size_t)s * part_floats(ne) + (size_t)(r % 16) * 16 * ne + e] * __shfl(f, s, 64);
@@ -486,9 +502,9 @@ __global__ __launch_bounds__(512, RWB == 128 ? 4 : 2) void k_attn_span_pp(AttnSp
   bf16x8_t qf[QT][NC];
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
-    const int r = min(q0 + 16 * t + l16, R - 1), i = r / a.G;
-    rows[t] = row_of(a, b, hk, r, i);
-    const uint16_t* qp = (const uint16_t*)a.q + (size_t)b * a.qb + (size_t)i * a.qr + (size_t)(hk * a.G + r % a.G) * a.qh;
+    const int r = min(q0 + 16 * t + l16, R - 1), i = query_of(a, r), h = r - i * a.G;
+    rows[t] = row_of(a, b, hk, h, i);
+    const uint16_t* qp = (const uint16_t*)a.q + (size_t)b * a.qb + (size_t)i * a.qr + (size_t)(hk * a.G + h) * a.qh;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       const int e = 32 * c + 8 * g;
@@ -507,19 +523,19 @@ __global__ __launch_bounds__(512, RWB == 128 ? 4 : 2) void k_attn_span_pp(AttnSp
     if (g == 0) *reinterpret_cast<i32x4_t*>(smem + kRows + (wave * 16 * QT + 16 * t + l16) * 16) = i32x4_t{rows[t].lo0, rows[t].n0, rows[t].lo1, rows[t].n1};
   }
   // the workgroup's tiles: those of the first hull, then those of the second beyond it, ascending
-  int t0, n0, t1, nt;
-  {
+  int t0 = 0, n0 = (a.n_k + KB - 1) / KB, t1 = 0, nt = n0;
+  if (a.n_spans) {
+    // (LDS waits only: the queries' loads stay in flight)
     int* const x = reinterpret_cast<int*>(smem);
-    if (lane == 0) {
-      x[wave * 4] = rg.h0; x[wave * 4 + 1] = rg.e0; x[wave * 4 + 2] = rg.h1; x[wave * 4 + 3] = rg.e1;
-    }
-    __syncthreads();
+    if (lane == 0) *reinterpret_cast<i32x4_t*>(x + wave * 4) = i32x4_t{rg.h0, rg.e0, rg.h1, rg.e1};
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     int h0 = 0x7fffffff, e0 = 0, h1 = 0x7fffffff, e1 = 0;
 #pragma unroll
     for (int w = 0; w < 8; ++w) {
-      h0 = min(h0, x[w * 4]); e0 = max(e0, x[w * 4 + 1]); h1 = min(h1, x[w * 4 + 2]); e1 = max(e1, x[w * 4 + 3]);
+      const i32x4_t y = *reinterpret_cast<const i32x4_t*>(x + w * 4);
+      h0 = min(h0, y[0]); e0 = max(e0, y[1]); h1 = min(h1, y[2]); e1 = max(e1, y[3]);
     }
-    __syncthreads();
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     int a0 = h0 / KB, b0 = (e0 + KB - 1) / KB, a1 = h1 / KB, b1 = (e1 + KB - 1) / KB;
     if (e0 <= 0) a0 = b0 = 0;
     if (e1 <= 0) a1 = b1 = 0;
@@ -531,7 +547,6 @@ __global__ __launch_bounds__(512, RWB == 128 ? 4 : 2) void k_attn_span_pp(AttnSp
     t1 = __builtin_amdgcn_readfirstlane(a1);
     nt = __builtin_amdgcn_readfirstlane(b0 - a0 + b1 - a1);
   }
-  auto tile_of = [&](int j) __attribute__((always_inline)) { return j < n0 ? t0 + j : t1 + j - n0; };
   const char* const kp = (const char*)a.k + ((size_t)b * a.kb + (size_t)hk * a.kh) * 2;
   const char* const vp = (const char*)a.v + ((size_t)b * a.vb + (size_t)hk * a.vh) * 2;
   // the rows of an LDS tile are rotated by f(row) among their 16-byte chunks, so that both the
@@ -548,23 +563,37 @@ __global__ __launch_bounds__(512, RWB == 128 ? 4 : 2) void k_attn_span_pp(AttnSp
     vok[j] = e < d ? (uint32_t)row * (uint32_t)a.kr * 2u + (uint32_t)e * 2u : 0x80000000u;
     vov[j] = e < d ? (uint32_t)row * (uint32_t)a.vr * 2u + (uint32_t)e * 2u : 0x80000000u;
   }
-  // DMA of tile number *j of the walk into ring slot *slot.  The tile's resource ends with the last key's
-  // last element, so that keys past it, and tiles past the walk, load as zeros (or, with a stride
-  // below d, as elements of the last keys: their probabilities are zero)
-  auto load = [&](const char* base, int64_t ld, const uint32_t (&vo)[DPW], int off, int* j, int* slot) __attribute__((always_inline)) {
-    const int tile = tile_of(*j), left = *j < nt ? min(a.n_k - tile * KB, KB) : 0;
-    const uint32_t num = left > 0 ? (uint32_t)((left - 1) * ld + d) * 2u : 0u;
-    __amdgpu_buffer_rsrc_t rs =
-        __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base) + (left > 0 ? (size_t)tile * KB * ld * 2 : 0), 0, num, 0x00020000);
+  // The walk over K's and V's tiles: the next tile's address, its keys up to the last, its number and
+  // its ring slot, advanced tile by tile; what happens once or at the end is branched to (formed
+  // anew for each tile, with selects, this took 100 scalar instructions of the softmax slot).
+  struct Walk { const char* p; int left, j, slot; };
+  const uint32_t kl = (uint32_t)a.kr * 2u, vl = (uint32_t)a.vr * 2u, fullk = (KB - 1) * kl + d * 2, fullv = (KB - 1) * vl + d * 2;
+  Walk wk{kp + (size_t)t0 * KB * kl, a.n_k - t0 * KB, 0, 0}, wv{vp + (size_t)t0 * KB * vl, a.n_k - t0 * KB, 0, 0};
+  // DMA of the walk's next tile.  The tile's resource ends with the last key's last element, so that
+  // keys past it load as zeros (or, with a stride below d, as elements of the last keys: their
+  // probabilities are zero); tiles past the walk are read too, as far as there are keys, and not used
+  auto load = [&](Walk& w, const char* base, uint32_t ld, uint32_t full, const uint32_t (&vo)[DPW], int off) __attribute__((always_inline)) {
+    uint32_t num = full;
+    if (__builtin_expect(w.left < KB, 0)) {
+      asm volatile("");
+      num = w.left > 0 ? (uint32_t)(w.left - 1) * ld + d * 2 : 0u;
+    }
+    __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(w.p), 0, num, 0x00020000);
 #pragma unroll
     for (int i = 0; i < DPW; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, FF_AS3(smem + off + *slot + (wave * DPW + i) * 1024), 16, vo[i], 0, 0, 0);
-    ++*j;
-    *slot = *slot == (NB - 1) * TB ? 0 : *slot + TB;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, FF_AS3(smem + off + w.slot + (wave * DPW + i) * 1024), 16, vo[i], 0, 0, 0);
+    ++w.j;
+    w.left -= KB;
+    w.p += (size_t)KB * ld;
+    if (__builtin_expect(w.j == n0, 0)) {   // on to the second range
+      asm volatile("");
+      w.left = a.n_k - t1 * KB;
+      w.p = base + (size_t)t1 * KB * ld;
+    }
+    w.slot = (w.slot + TB) & (NB * TB - 1);
   };
-  int ktile = 0, vtile = 0, kslot = 0, vslot = 0;
-  auto load_k = [&]() __attribute__((always_inline)) { load(kp, a.kr, vok, 0, &ktile, &kslot); };
-  auto load_v = [&]() __attribute__((always_inline)) { load(vp, a.vr, vov, NB * TB, &vtile, &vslot); };
+  auto load_k = [&]() __attribute__((always_inline)) { load(wk, kp, kl, fullk, vok, 0); };
+  auto load_v = [&]() __attribute__((always_inline)) { load(wv, vp, vl, fullv, vov, NB * TB); };
   // fragment addresses within a tile (k step c and output tile e enter by xor)
   const uint32_t lds0 = (uint32_t)(uintptr_t)((__attribute__((address_space(3))) const void*)smem);
   const uint32_t ka = lds0 + l16 * RWB + ((g ^ swz(l16)) * 16);
@@ -715,13 +744,13 @@ __global__ __launch_bounds__(512, RWB == 128 ? 4 : 2) void k_attn_span_pp(AttnSp
         }
   };
   // sc -> probabilities pb (complete when it returns: nothing of it moves past the barrier)
-  auto softmax = [&](int k0, bool some, bool part) __attribute__((always_inline)) {
-    if (!some) {
+  auto softmax = [&](int k0, bool all, bool some) __attribute__((always_inline)) {
+    if (!all && !some) {
 #pragma unroll
       for (int t = 0; t < QT; ++t) pb[0][t] = pb[1][t] = __builtin_bit_cast(bf16x8_t, u32x4_t{0u, 0u, 0u, 0u});
     } else {
       if constexpr (MOD) modify(k0);
-      if (part) {
+      if (!all) {
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
           const i32x4_t w = spans_at(t);
@@ -783,6 +812,8 @@ __global__ __launch_bounds__(512, RWB == 128 ? 4 : 2) void k_attn_span_pp(AttnSp
     for (int t = 0; t < QT; ++t) { FF_TIE(pb[0][t]); FF_TIE(pb[1][t]); FF_TIE(l[t]); }
     __builtin_amdgcn_sched_barrier(0);
   };
+  // tiles that start in [c, c + core) lie in a core as a whole
+  const unsigned core0 = max(rg.d0 - rg.c0 - KB + 1, 0), core1 = max(rg.d1 - rg.c1 - KB + 1, 0);
   bool mixed = false;   // some tile held keys that a row does not see
   if (nt > 0) {
     load_k();
@@ -795,14 +826,18 @@ __global__ __launch_bounds__(512, RWB == 128 ? 4 : 2) void k_attn_span_pp(AttnSp
     drain();
     ks = TB;
     if (wave >= 4) FF_BAR();   // the second group runs one slot behind
+    int k0 = t0 * KB;
     for (int j = 0; j < nt; ++j) {
-      const int k0 = tile_of(j) * KB;
-      const bool some = rg.some(k0, KB), part = some && !rg.all(k0, KB);
-      mixed = mixed || part || !some;
       load_k();
       load_v();
       __builtin_amdgcn_sched_barrier(0);
-      softmax(k0, some, part);
+      const bool all = (unsigned)(k0 - rg.c0) < core0 || (unsigned)(k0 - rg.c1) < core1;
+      bool some = false;
+      if (!all) {
+        some = rg.some(k0, KB);
+        mixed = true;
+      }
+      softmax(k0, all, some);
       ka_ = ka + ks;
       va_ = va + vs;
       static_for<0, UD>(rd);
@@ -812,8 +847,13 @@ __global__ __launch_bounds__(512, RWB == 128 ? 4 : 2) void k_attn_span_pp(AttnSp
       static_for<0, UK + UV>(unit);
       __builtin_amdgcn_s_setprio(0);
       FF_BAR();
-      ks = ks == (NB - 1) * TB ? 0 : ks + TB;
-      vs = vs == (NB - 1) * TB ? 0 : vs + TB;
+      ks = (ks + TB) & (NB * TB - 1);
+      vs = (vs + TB) & (NB * TB - 1);
+      k0 += KB;
+      if (__builtin_expect(j + 1 == n0, 0)) {
+        asm volatile("");
+        k0 = t1 * KB;
+      }
     }
     wait_vm<0>();
     if (wave < 4) FF_BAR();
@@ -826,19 +866,22 @@ __global__ __launch_bounds__(512, RWB == 128 ? 4 : 2) void k_attn_span_pp(AttnSp
   if (mixed) {
     Top top;
 #pragma unroll
-    for (int e = 0; e < NE; ++e)
+    for (int t = 0; t < QT; ++t) {
+      const i32x4_t w = spans_at(t);
+      if (w[1] == 0 && w[3] == 0) continue;
 #pragma unroll
-      for (int t = 0; t < QT; ++t)
+      for (int e = 0; e < NE; ++e)
 #pragma unroll
         for (int v = 0; v < 4; ++v) top.f32(o[e][t][v]);
+    }
     if (__builtin_expect(__any(top.odd()), 0)) {
       static_assert(kKeys * (NE * 32 + 16) * 8 <= kRows, "a wavefront's staged V rows");
 #pragma unroll
       for (int t = 0; t < QT; ++t) {
-        const int r = min(q0 + 16 * t + l16, R - 1), i = r / a.G;
-        const Row w[1] = {row_of(a, b, hk, r, i)};
+        const int r = min(q0 + 16 * t + l16, R - 1), i = query_of(a, r), h = r - i * a.G;
+        const Row w[1] = {row_of(a, b, hk, h, i)};
         const Ranges rt = ranges_of<1>(w);
-        const char* qp = (const char*)((const uint16_t*)a.q + (size_t)b * a.qb + (size_t)i * a.qr + (size_t)(hk * a.G + r % a.G) * a.qh);
+        const char* qp = (const char*)((const uint16_t*)a.q + (size_t)b * a.qb + (size_t)i * a.qr + (size_t)(hk * a.G + h) * a.qh);
         const int end = max(rt.e0, rt.e1);
         f32x4_t x[NE];
         attend16<DT_BF16, NE>(a, w[0], rt, qp, kp, vp, end > 0 ? min(rt.h0, rt.h1) & ~(kKeys - 1) : 0, end, kKeys,
@@ -855,18 +898,21 @@ __global__ __launch_bounds__(512, RWB == 128 ? 4 : 2) void k_attn_span_pp(AttnSp
   for (int t = 0; t < QT; ++t) {
     float s = l[t] + __shfl_xor(l[t], 16, 64);
     s += __shfl_xor(s, 32, 64);
-    const float inv = s == 0.f ? 0.f : 1.0f / s;   // no key seen: zeros
+    const i32x4_t w = spans_at(t);
+    const bool none = s == 0.f || (w[1] == 0 && w[3] == 0);   // no key seen: zeros, whatever has been formed
+    const float inv = 1.0f / s;
 #pragma unroll
-    for (int e = 0; e < NE; ++e)
-      *reinterpret_cast<u32x2_t*>(stg + (16 * t + l16) * LDO + 16 * e + 4 * g) =
-          u32x2_t{pack_bf16x2(o[e][t][0] * inv, o[e][t][1] * inv), pack_bf16x2(o[e][t][2] * inv, o[e][t][3] * inv)};
+    for (int e = 0; e < NE; ++e) {
+      const u32x2_t y = {pack_bf16x2(o[e][t][0] * inv, o[e][t][1] * inv), pack_bf16x2(o[e][t][2] * inv, o[e][t][3] * inv)};
+      *reinterpret_cast<u32x2_t*>(stg + (16 * t + l16) * LDO + 16 * e + 4 * g) = none ? u32x2_t{0u, 0u} : y;
+    }
   }
   uint16_t* out = reinterpret_cast<uint16_t*>(a.out) + (size_t)b * a.ob;
   const int ppr = d / 8;
   for (int idx = lane; idx < 16 * QT * ppr; idx += 64) {
-    const int row = idx / ppr, pc = idx - row * ppr, r = q0 + row;
+    const int row = idx / ppr, pc = idx - row * ppr, r = q0 + row, i = query_of(a, r);
     if (r < R)
-      *reinterpret_cast<u32x4_t*>(out + (size_t)(r / a.G) * a.orow + (size_t)(hk * a.G + r % a.G) * a.oh + pc * 8) =
+      *reinterpret_cast<u32x4_t*>(out + (size_t)i * a.orow + (size_t)(hk * a.G + r - i * a.G) * a.oh + pc * 8) =
           *reinterpret_cast<const u32x4_t*>(stg + row * LDO + pc * 8);
   }
 #endif
@@ -914,8 +960,11 @@ size_t attention_span_workspace(int, int B, int H_kv, int G, int d, int n_q, int
   return n > 1 ? (size_t)t * n * part_floats(pieces(d)) * 4 : 0;
 }
 
-hipError_t attention_span(int dtype, const AttnSpanArgs& a, hipStream_t s) {
-  if (a.n_q <= 0) return hipSuccess;
+hipError_t attention_span(int dtype, const AttnSpanArgs& args, hipStream_t s) {
+  if (args.n_q <= 0) return hipSuccess;
+  AttnSpanArgs a = args;
+  while ((1L << a.gshift) < a.G) ++a.gshift;
+  a.gmul = (uint32_t)(((1ull << (31 + a.gshift)) + a.G - 1) / a.G);
   const long t = tiles16(a.B, a.H_kv, a.G, a.n_q);
   if (dtype == DT_BF16 && (long)a.n_q * a.G > 64) return launch_pp(a, s);
   const int n = splits(t, a.n_k), ne = pieces(a.d);

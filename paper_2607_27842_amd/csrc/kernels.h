@@ -188,6 +188,7 @@ struct AttnSpanArgs {
   float scale, cap;
   int bias_kind, reach; const float* bias; const int32_t* pos;
   const int32_t* spans; int n_spans; int64_t span_batch;
+  uint32_t gmul; int gshift;   // r / G = r gmul >> 31 + gshift (set by attention_span)
   float* part;   // workspace: attention_span_workspace bytes
 };
 size_t attention_span_workspace(int dtype, int B, int H_kv, int G, int d, int n_q, int n_k);

@@ -245,7 +245,7 @@ ff_status ff_attention(const ff_attn_desc* d, const void* q, const void* k, cons
   CHECK(!eo.meets(ew), FF_E_SHAPE, "out overlaps the workspace");
   const AttnSpanArgs a{q, k, v, out, d->q_batch, d->q_row, d->q_head, d->k_batch, d->k_row, d->k_head, d->v_batch, d->v_row,
                        d->v_head, d->o_batch, d->o_row, d->o_head, d->B, d->H_kv, d->H / d->H_kv, d->d, d->n_q, d->n_k,
-                       d->scale, d->cap, d->bias_kind, d->bias_reach, bias, pos, spans, d->n_spans, d->span_batch,
+                       d->scale, d->cap, d->bias_kind, d->bias_reach, bias, pos, spans, d->n_spans, d->span_batch, 0, 0,
                        need ? (float*)ws : nullptr};
   HIP_TRY(attention_span(d->dtype, a, reinterpret_cast<hipStream_t>(stream)), "attention over spans");
   return ok();

@@ -81,22 +81,36 @@ __device__ __forceinline__ Ranges ranges_of(const Row (&w)[QT]) {
   return r;
 }
 
-// The score of key k from the product x = q . k: natural units in fp32, log2 units in bf16 (where its
-// exponential is the hardware's exp2 and tanh is formed from exp2 and rcp, a few 1e-7 of the cap
-// off, far below a bf16 probability's rounding).  A finite score stays finite: the type's lowest
-// value in a table is a score like any other.
+// The scores of 8 keys from the products p = q . k, key j at k0 + 16 (j / 4) + j % 4: natural units in fp32,
+// log2 units in bf16 (where the exponential is the hardware's exp2 and tanh is formed from exp2 and
+// rcp, a few 1e-7 of the cap off, far below a bf16 probability's rounding).  A finite score stays
+// finite: the type's lowest value in a table is a score like any other.
 template <bool F32>
-__device__ __forceinline__ float score(const AttnSpanArgs& a, const Row& w, float x, int k) {
-  float t = x * a.scale;
+__device__ __forceinline__ void scores(const AttnSpanArgs& a, const Row& w, float (&p)[8], int k0) {
   if (a.cap > 0.f) {
-    const float y = t / a.cap;
-    t = a.cap * (F32 ? tanhf(y) : 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(2.f * kLog2e * y)));
+    const float c1 = F32 ? a.scale / a.cap : 2.f * kLog2e * a.scale / a.cap, c2 = a.cap;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      p[j] = F32 ? c2 * tanhf(c1 * p[j]) : fmaf(-2.f * c2, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(c1 * p[j])), c2);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) p[j] *= a.scale;
   }
-  if (a.bias_kind == BIAS_SLOPE) t -= w.bias[0] * fabsf((float)(k - w.pos));
-  else if (a.bias_kind == BIAS_TABLE) t += w.bias[min(max(k - w.pos, -a.reach), a.reach)];
-  if (F32) return t;
-  const float u = t * kLog2e;
-  return fabsf(t) <= kFltMax ? fminf(fmaxf(u, -kFltMax), kFltMax) : u;
+  if (a.bias_kind == BIAS_SLOPE) {
+    const float slope = w.bias[0];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) p[j] -= slope * fabsf((float)(k0 + 16 * (j / 4) + j % 4 - w.pos));
+  } else if (a.bias_kind == BIAS_TABLE) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) p[j] += w.bias[min(max(k0 + 16 * (j / 4) + j % 4 - w.pos, -a.reach), a.reach)];
+  }
+  if (!F32) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float u = p[j] * kLog2e;
+      p[j] = fabsf(p[j]) <= kFltMax ? fminf(fmaxf(u, -kFltMax), kFltMax) : u;
+    }
+  }
 }
 template <bool F32>
 __device__ __forceinline__ float exp_of(float t) { return F32 ? expf(t) : __builtin_amdgcn_exp2f(t); }
@@ -166,45 +180,52 @@ __device__ __forceinline__ void attend16(const AttnSpanArgs& a, const Row& w, co
     const int e = DQ * c + EQ * g;
     qf[c] = e < d ? *reinterpret_cast<const u32x4_t*>(qp + e * es) : zu;
   }
-  // Keys past the end read the last one (their scores are masked), dims past d the row's first (of K
-  // they count as zeros, of V their products are never stored): no load depends on a lane's mask.
+  // A step's loads go through resources that end with its last key's last element: keys past it load
+  // as zeros (or, with a stride below d, as elements of the last keys), and so do dims past d.
+  constexpr uint32_t kOut = 0x80000000u;
+  const uint32_t kl = (uint32_t)a.kr * (uint32_t)es, vl = (uint32_t)a.vr * (uint32_t)es;
+  constexpr int NT = NQ > 2 ? 2 : NQ;           // the last chunks, where d may end
+  constexpr bool kStep = !F32 && CPR == 16;     // chunks j lie 4 j rows further
+  uint32_t ko[2], kt[2][NT], vo[F32 ? 4 : kStep ? 1 : NV], vt0 = 0;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    ko[i] = (16 * i + l16) * kl + EQ * g * (uint32_t)es;
+#pragma unroll
+    for (int c = 0; c < NT; ++c) {
+      const int e = DQ * (NQ - NT + c);
+      kt[i][c] = e + EQ * g < d ? ko[i] + e * (uint32_t)es : kOut;
+    }
+  }
+  if constexpr (F32) {
+#pragma unroll
+    for (int v = 0; v < 4; ++v) vo[v] = (4 * g + v) * vl + l16 * 4u;
+    vt0 = 16 * vl;
+  } else {
+#pragma unroll
+    for (int j = 0; j < (kStep ? 1 : NV); ++j) {
+      const int idx = j * 64 + lane, e = idx % CPR * 8;
+      vo[j] = e < d ? (idx / CPR) * vl + e * 2u : kOut;
+    }
+  }
   auto load = [&](int k0) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const char* row = kp + (size_t)min(k0 + 16 * i + l16, end - 1) * a.kr * es;
-#pragma unroll
-      for (int c = 0; c < NQ; ++c) {
-        const int e = DQ * c + EQ * g;
-        kf[i][c] = *reinterpret_cast<const u32x4_t*>(row + (c < NQ - 2 || e < d ? e : 0) * es);
-      }
-    }
-    if constexpr (F32) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const char* row = vp + (size_t)min(k0 + 16 * (j / 4) + 4 * g + j % 4, end - 1) * a.vr * 4;
-#pragma unroll
-        for (int c = 0; c < NE; ++c) {
-          const int e = 16 * c + l16;
-          vv[j][c] = *reinterpret_cast<const float*>(row + (c < NE - 2 || e < d ? e : 0) * 4);
-        }
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const int idx = j * 64 + lane, e = idx % CPR * 8;
-        vf[j] = *reinterpret_cast<const u32x4_t*>(vp + ((size_t)min(k0 + idx / CPR, end - 1) * a.vr + (e < d ? e : 0)) * 2);
-      }
-    }
-  };
-  const bool whole = d == DQ * NQ;
-  auto cut = [&]() __attribute__((always_inline)) {
-    if (whole) return;
+    const uint32_t last = min(end - k0, kKeys) - 1;
+    __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(kp) + (size_t)k0 * kl, 0, last * kl + d * (int)es, 0x00020000);
+    __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(vp) + (size_t)k0 * vl, 0, last * vl + d * (int)es, 0x00020000);
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int c = NQ > 2 ? NQ - 2 : 0; c < NQ; ++c)
+      for (int c = 0; c < NQ; ++c)
+        kf[i][c] = __builtin_amdgcn_raw_buffer_load_b128(rk, c < NQ - NT ? ko[i] + c * DQ * (int)es : kt[i][c < NQ - NT ? 0 : c - (NQ - NT)], 0, 0);
+    if constexpr (F32) {
 #pragma unroll
-        for (int x = 0; x < 4; ++x) kf[i][c][x] = DQ * c + EQ * g < d ? kf[i][c][x] : 0u;
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int c = 0; c < NE; ++c)   // dims past d: what lies there, or zeros; never stored
+          vv[j][c] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rv, vo[j % 4] + (j / 4) * vt0 + c * 64, 0, 0));
+    } else {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) vf[j] = __builtin_amdgcn_raw_buffer_load_b128(rv, kStep ? vo[0] + j * 4 * vl : vo[kStep ? 0 : j], 0, 0);
+    }
   };
 #pragma unroll
   for (int e = 0; e < NE; ++e) o[e] = z4;
@@ -257,7 +278,6 @@ __device__ __forceinline__ void attend16(const AttnSpanArgs& a, const Row& w, co
       }
     }
     f32x4_t sc[2] = {z4, z4};
-    cut();
 #pragma unroll
     for (int c = 0; c < NQ; ++c)
 #pragma unroll
@@ -270,14 +290,20 @@ __device__ __forceinline__ void attend16(const AttnSpanArgs& a, const Row& w, co
           sc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[i][c]), __builtin_bit_cast(bf16x8_t, qf[c]), sc[i], 0, 0, 0);
         }
       }
+    const int kk = k0;
+    k0 = next(k0 + stride);
+    if constexpr (!F32)
+      if (k0 < end) load(k0);   // K is in the scores, V in LDS
     float p[8], x = -INFINITY;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int k = k0 + 16 * (j / 4) + 4 * g + j % 4;
-      p[j] = score<F32>(a, w, sc[j / 4][j % 4], k);
-      if (part && !w.sees(k)) p[j] = -INFINITY;
-      x = fmaxf(x, p[j]);
+    for (int j = 0; j < 8; ++j) p[j] = sc[j / 4][j % 4];
+    scores<F32>(a, w, p, kk + 4 * g);
+    if (part) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) p[j] = w.sees(kk + 16 * (j / 4) + 4 * g + j % 4) ? p[j] : -INFINITY;
     }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x = fmaxf(x, p[j]);
     x = fmaxf(x, __shfl_xor(x, 16, 64));
     x = fmaxf(x, __shfl_xor(x, 32, 64));
     const float mn = fmaxf(m, x), mo = mn == -INFINITY ? 0.f : mn;
@@ -297,7 +323,7 @@ __device__ __forceinline__ void attend16(const AttnSpanArgs& a, const Row& w, co
 #pragma unroll
         for (int c = 0; c < NE; ++c) o[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(vv[j][c], p[j], o[c], 0, 0, 0);
       if (__builtin_expect(odd, 0)) {
-        for (int k = k0; k < min(k0 + kKeys, end); ++k)
+        for (int k = kk; k < min(kk + kKeys, end); ++k)
 #pragma unroll
           for (int c = 0; c < NE; ++c) {
             if (16 * c + 4 * g >= d) continue;
@@ -307,26 +333,29 @@ __device__ __forceinline__ void attend16(const AttnSpanArgs& a, const Row& w, co
               if (odd_f32(y[e]) && w.sees(k)) o[c][e] += y[e];
           }
       }
-      k0 = next(k0 + stride);
       if (k0 < end) load(k0);
     } else {
-      const int kk = k0;
-      k0 = next(k0 + stride);
-      if (k0 < end) load(k0);
       const u32x4_t pw = {pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])};
-      u32x2_t vt[NE][2];
+      // in two halves, for the registers
+      constexpr int NH = (NE + 1) / 2;
 #pragma unroll
-      for (int e = 0; e < NE; ++e) {
-        vt[e][0] = lds_rd64_tr(va, e * 32);
-        vt[e][1] = lds_rd64_tr(va, e * 32 + 16 * PV);
-      }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      for (int h = 0; h < NE; h += NH) {
+        u32x2_t vt[NH][2];
 #pragma unroll
-      for (int e = 0; e < NE; ++e) {
-        FF_TIE(vt[e][0]);
-        FF_TIE(vt[e][1]);
-        const u32x4_t vw = {vt[e][0][0], vt[e][0][1], vt[e][1][0], vt[e][1][1]};
-        o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, vw), __builtin_bit_cast(bf16x8_t, pw), o[e], 0, 0, 0);
+        for (int e = 0; e < NH; ++e)
+          if (h + e < NE) {
+            vt[e][0] = lds_rd64_tr(va, (h + e) * 32);
+            vt[e][1] = lds_rd64_tr(va, (h + e) * 32 + 16 * PV);
+          }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int e = 0; e < NH; ++e)
+          if (h + e < NE) {
+            FF_TIE(vt[e][0]);
+            FF_TIE(vt[e][1]);
+            const u32x4_t vw = {vt[e][0][0], vt[e][0][1], vt[e][1][0], vt[e][1][1]};
+            o[h + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, vw), __builtin_bit_cast(bf16x8_t, pw), o[h + e], 0, 0, 0);
+          }
       }
       if (__builtin_expect(odd, 0)) {
         for (int k = kk; k < min(kk + kKeys, end); ++k)
@@ -353,7 +382,7 @@ __device__ __forceinline__ void attend16(const AttnSpanArgs& a, const Row& w, co
 
 // 16 rows a workgroup, whose 4 waves take every fourth step of 32 keys.
 template <int DT, int NE>
-__global__ __launch_bounds__(256) void k_attn_dir(AttnSpanArgs a, int nsplit) {
+__global__ __launch_bounds__(256, 2) void k_attn_dir(AttnSpanArgs a, int nsplit) {
 #ifdef __HIP_DEVICE_COMPILE__   // the host pass needs the launch stub only
   constexpr bool F32 = DT == DT_F32;
   constexpr int PV = NE * 32 + 16;              // bf16: bytes of a staged V row
@@ -430,34 +459,47 @@ __global__ __launch_bounds__(256) void k_attn_dir(AttnSpanArgs a, int nsplit) {
 #endif
 }
 
-// Joins the splits of a row, a wavefront each: out = sum_s O_s e^(m_s - m) / sum_s l_s e^(m_s - m)
+// Joins the splits of a row, a workgroup each: out = sum_s O_s e^(m_s - m) / sum_s l_s e^(m_s - m).
+// 8 groups of 32 lanes take every eighth split, 4 dims a lane, so that a lane's loads (at most 8) are in
+// flight together (one wavefront walking up to 64 splits took 35 us of a call's 50).
 template <int DT>
 __global__ __launch_bounds__(256) void k_attn_join(AttnSpanArgs a, int nsplit, int ne) {
-  const int lane = threadIdx.x & 63;
-  const int R = a.n_q * a.G, nt = (R + 15) / 16;
-  const long row = (long)blockIdx.x * 4 + (threadIdx.x >> 6);   // (b, hk, r)
-  if (row >= (long)a.B * a.H_kv * R) return;
-  const int r = (int)(row % R), bh = (int)(row / R), hk = bh % a.H_kv, b = bh / a.H_kv;
-  const float* pt = a.part + ((size_t)bh * nt + r / 16) * nsplit * part_floats(ne);
-  const float* ml = pt + 256 * ne + 2 * (r % 16);
-  // lane s < nsplit (at most 64) holds split s's statistics
-  float ms = -INFINITY, ls = 0.f;
-  if (lane < nsplit) {
-    ms = ml[(size_t)lane * part_floats(ne)];
-    ls = ml[(size_t)lane * part_floats(ne) + 1];
+  __shared__ float f[kMaxSplit], linv;
+  __shared__ f32x4_t part[8][32];
+  const int tid = threadIdx.x, lane = tid & 63, q = tid & 31, grp = tid >> 5;
+  const int R = a.n_q * a.G, nt = (R + 15) / 16, pf = part_floats(ne);
+  const int r = blockIdx.x % R, bh = blockIdx.x / R, hk = bh % a.H_kv, b = bh / a.H_kv;
+  const float* pt = a.part + ((size_t)bh * nt + r / 16) * nsplit * pf;
+  const float* row = pt + (r % 16) * 16 * ne + 4 * q;
+  f32x4_t x[kMaxSplit / 8];
+  const bool in = 4 * q < a.d;
+#pragma unroll
+  for (int i = 0; i < kMaxSplit / 8; ++i) {
+    const int s = 8 * i + grp;
+    x[i] = in && s < nsplit ? *reinterpret_cast<const f32x4_t*>(row + (size_t)s * pf) : f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
-  float m = ms;   // a NaN statistic makes its weight, and so the row, NaN
-  m = wave_max(m);
-  const float f = exp_of<DT == DT_F32>(ms - (m == -INFINITY ? 0.f : m));
-  const float l = wave_sum(ls * f);
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+  if (tid < 64) {   // lane s holds split s's statistics; a NaN sum makes the row NaN
+    float ms = -INFINITY, ls = 0.f;
+    if (lane < nsplit) {
+      ms = pt[(size_t)lane * pf + 256 * ne + 2 * (r % 16)];
+      ls = pt[(size_t)lane * pf + 256 * ne + 2 * (r % 16) + 1];
+    }
+    const float m = wave_max(ms), w = exp_of<DT == DT_F32>(ms - (m == -INFINITY ? 0.f : m)), l = wave_sum(ls * w);
+    f[lane] = w;
+    if (lane == 0) linv = l == 0.f ? 0.f : 1.f / l;
+  }
+  __syncthreads();
+  f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < kMaxSplit / 8; ++i)
+    if (8 * i + grp < nsplit) o += x[i] * f[8 * i + grp];
+  part[grp][q] = o;
+  __syncthreads();
+  if (tid >= 32 || !in) return;
+#pragma unroll
+  for (int i = 1; i < 8; ++i) o += part[i][q];
   const int qi = query_of(a, r);
-  const size_t oo = (size_t)b * a.ob + (size_t)qi * a.orow + (size_t)(hk * a.G + r - qi * a.G) * a.oh;
-  for (int e = lane; e < a.d; e += 64) {
-    float x = 0.f;
-    for (int s = 0; s < nsplit; ++s) x += pt[(size_t)s * part_floats(ne) + (size_t)(r % 16) * 16 * ne + e] * __shfl(f, s, 64);
-    St<DT>::st1(a.out, oo + e, x * inv);
-  }
+  store_o4<DT>(a.out, (size_t)b * a.ob + (size_t)qi * a.orow + (size_t)(hk * a.G + r - qi * a.G) * a.oh + 4 * q, o * linv);
 }
 
 // ---------------------------------------------------------------- bf16, many rows: two wave groups in turn
@@ -988,8 +1030,8 @@ hipError_t attention_span(int dtype, const AttnSpanArgs& args, hipStream_t s) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || n == 1) return e;
   const long rows = (long)a.B * a.H_kv * a.n_q * a.G;
-  if (dtype == DT_BF16) FF_LAUNCH(k_attn_join<DT_BF16>, (unsigned)((rows + 3) / 4), 256, 0, s, a, n, ne);
-  else FF_LAUNCH(k_attn_join<DT_F32>, (unsigned)((rows + 3) / 4), 256, 0, s, a, n, ne);
+  if (dtype == DT_BF16) FF_LAUNCH(k_attn_join<DT_BF16>, (unsigned)rows, 256, 0, s, a, n, ne);
+  else FF_LAUNCH(k_attn_join<DT_F32>, (unsigned)rows, 256, 0, s, a, n, ne);
   return hipGetLastError();
 }
 

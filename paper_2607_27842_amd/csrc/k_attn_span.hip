@@ -994,12 +994,29 @@ hipError_t launch_pp(const AttnSpanArgs& a, hipStream_t s) {
 }
 long tiles16(int B, int H_kv, int G, int n_q) { return (long)B * H_kv * (((long)n_q * G + 15) / 16); }
 
-}  // namespace
-
-size_t attention_span_workspace(int, int B, int H_kv, int G, int d, int n_q, int n_k) {
+// The splits of the direct kernel's keys, or 0 for k_attn_span_pp, by estimated time (us; all keys seen),
+// fitted to 1 to 16 heads of 64 and 128, 16 to 1000 tokens, B 1 to 8.  The direct kernel: 1.9 for each 128
+// keys of a workgroup or 6.5e-3 for each of all workgroups' together; k_attn_span_pp: 1.1 (0.8 for d <= 64)
+// for each 64 keys and round of workgroups.
+//   B = 1, 16 heads of 128: 33 tokens 5.9 against 8.2 us, 256 tokens 9.0 against 10.3, 640 26 against 16
+//   B = 4, 16 heads of 128: 64 tokens 6.1 against 7.6, 128 tokens 10.8 against 8.8, 1000 163 against 44
+int plan(int dtype, int B, int H_kv, int G, int d, int n_q, int n_k) {
   const long t = tiles16(B, H_kv, G, n_q);
   const int n = splits(t, n_k);
-  return n > 1 ? (size_t)t * n * part_floats(pieces(d)) * 4 : 0;
+  if (dtype == DT_F32) return n;
+  const double turns = (double)((n_k + 127) / 128), chain = 1.9 * turns / n, work = 6.5e-3 * t * turns;
+  const double dir = 5.0 + (chain > work ? chain : work) + (n > 1 ? 5.0 : 0.0);
+  const long wg = (long)B * H_kv * (((long)n_q * G + 127) / 128), at_once = d <= 64 ? 512 : 256;
+  const double pp = 6.3 + (d <= 64 ? 0.8 : 1.1) * ((n_k + 63) / 64) * ((wg + at_once - 1) / at_once);
+  return dir <= pp ? n : 0;
+}
+
+}  // namespace
+
+size_t attention_span_workspace(int dtype, int B, int H_kv, int G, int d, int n_q, int n_k) {
+  if (n_q <= 0) return 0;
+  const int n = plan(dtype, B, H_kv, G, d, n_q, n_k);
+  return n > 1 ? (size_t)tiles16(B, H_kv, G, n_q) * n * part_floats(pieces(d)) * 4 : 0;
 }
 
 hipError_t attention_span(int dtype, const AttnSpanArgs& args, hipStream_t s) {
@@ -1008,8 +1025,8 @@ hipError_t attention_span(int dtype, const AttnSpanArgs& args, hipStream_t s) {
   while ((1L << a.gshift) < a.G) ++a.gshift;
   a.gmul = (uint32_t)(((1ull << (31 + a.gshift)) + a.G - 1) / a.G);
   const long t = tiles16(a.B, a.H_kv, a.G, a.n_q);
-  if (dtype == DT_BF16 && (long)a.n_q * a.G > 64) return launch_pp(a, s);
-  const int n = splits(t, a.n_k), ne = pieces(a.d);
+  const int n = plan(dtype, a.B, a.H_kv, a.G, a.d, a.n_q, a.n_k), ne = pieces(a.d);
+  if (n == 0) return launch_pp(a, s);
   if (t * n > 0x7fffffffL) return hipErrorInvalidValue;
 #define FF_DIR(DT, NE) FF_LAUNCH((k_attn_dir<DT, NE>), (unsigned)(t * n), 256, 0, s, a, n)
 #define FF_DIR_D(DT)                   \

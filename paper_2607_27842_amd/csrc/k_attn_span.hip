@@ -522,7 +522,9 @@ __global__ __launch_bounds__(512, RWB == 128 ? 4 : 2) void k_attn_span_pp(AttnSp
   constexpr int CPR = RWB / 16;                  // 16-byte chunks per LDS row
   static_assert(NC * 64 <= RWB && NE * 32 <= RWB, "head dim tiles fit the LDS row");
   constexpr int LDO = NE * 16 + 8;               // staged output row pitch (elements)
-  constexpr int kMain = 2 * NB * TB, kOut = 8 * 16 * QT * LDO * 2;
+  // after the walk each wavefront has a region of its own, for V rows (attend16) and for its output
+  constexpr int kOwn = kKeys * (NE * 32 + 16) > 16 * QT * LDO * 2 ? kKeys * (NE * 32 + 16) : 16 * QT * LDO * 2;
+  constexpr int kMain = 2 * NB * TB, kOut = 8 * kOwn;
   constexpr float kPLim = 256.0f;                // as in k_attn_pp: what raises a row's running maximum
   constexpr int kRows = kMain > kOut ? kMain : kOut;   // behind it, the rows' spans (read where a tile needs a mask)
   __shared__ __attribute__((aligned(1024))) char smem[kRows + 128 * QT * 16];
@@ -917,7 +919,6 @@ __global__ __launch_bounds__(512, RWB == 128 ? 4 : 2) void k_attn_span_pp(AttnSp
         for (int v = 0; v < 4; ++v) top.f32(o[e][t][v]);
     }
     if (__builtin_expect(__any(top.odd()), 0)) {
-      static_assert(kKeys * (NE * 32 + 16) * 8 <= kRows, "a wavefront's staged V rows");
 #pragma unroll
       for (int t = 0; t < QT; ++t) {
         const int r = min(q0 + 16 * t + l16, R - 1), i = query_of(a, r), h = r - i * a.G;
@@ -927,7 +928,7 @@ __global__ __launch_bounds__(512, RWB == 128 ? 4 : 2) void k_attn_span_pp(AttnSp
         const int end = max(rt.e0, rt.e1);
         f32x4_t x[NE];
         attend16<DT_BF16, NE>(a, w[0], rt, qp, kp, vp, end > 0 ? min(rt.h0, rt.h1) & ~(kKeys - 1) : 0, end, kKeys,
-                              smem + wave * kKeys * (NE * 32 + 16), x, m[t], l[t]);
+                              smem + wave * kOwn, x, m[t], l[t]);
 #pragma unroll
         for (int e = 0; e < NE; ++e) o[e][t] = x[e];
       }
@@ -935,7 +936,7 @@ __global__ __launch_bounds__(512, RWB == 128 ? 4 : 2) void k_attn_span_pp(AttnSp
   }
   // o[e][t][v] = O[row q0 + 16 t + l16][16 e + 4 g + v], staged through the wave's own LDS
   // region and stored as 16-byte row pieces
-  uint16_t* stg = reinterpret_cast<uint16_t*>(smem) + wave * 16 * QT * LDO;
+  uint16_t* stg = reinterpret_cast<uint16_t*>(smem + wave * kOwn);
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     float s = l[t] + __shfl_xor(l[t], 16, 64);

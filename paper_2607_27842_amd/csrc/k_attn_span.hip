@@ -557,7 +557,8 @@ __global__ __launch_bounds__(512, RWB == 128 ? 4 : 2) void k_attn_span_pp(AttnSp
       qf[t][c] = __builtin_bit_cast(bf16x8_t, v);
     }
   }
-  const Ranges rg = ranges_of<QT>(rows);
+  Ranges rg{0, a.n_k, 0x7fffffff, 0, 0, a.n_k, 0, 0};
+  if (a.n_spans) rg = ranges_of<QT>(rows);
   int pos[QT];
   const float* bias[QT];
 #pragma unroll
@@ -722,9 +723,6 @@ __global__ __launch_bounds__(512, RWB == 128 ? 4 : 2) void k_attn_span_pp(AttnSp
     asm volatile("ds_read_b128 %0, %1 offset:%2\n\ts_waitcnt lgkmcnt(0)" : "=v"(w) : "v"(lds0 + kRows + (wave * 16 * QT + l16) * 16), "i"(t * 256) : "memory");
     return w;
   };
-  auto sees = [](i32x4_t w, int k) __attribute__((always_inline)) {
-    return (unsigned)(k - w[0]) < (unsigned)w[1] || (unsigned)(k - w[2]) < (unsigned)w[3];
-  };
   // a row's bias beyond the table's reach, on either side (log2 units)
   float below[MOD ? QT : 1], above[MOD ? QT : 1];
   if constexpr (MOD) {
@@ -798,11 +796,19 @@ __global__ __launch_bounds__(512, RWB == 128 ? 4 : 2) void k_attn_span_pp(AttnSp
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
           const i32x4_t w = spans_at(t);
+          const int at = k0 + 4 * g - w[0], at1 = k0 + 4 * g - w[2];
+          if (a.n_spans > 1) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int v = 0; v < 4; ++v)
-              sc[i][t][v] = sees(w, k0 + 16 * i + 4 * g + v) ? sc[i][t][v] : -INFINITY;
+              for (int v = 0; v < 4; ++v)
+                sc[i][t][v] = (unsigned)(at + 16 * i + v) < (unsigned)w[1] || (unsigned)(at1 + 16 * i + v) < (unsigned)w[3] ? sc[i][t][v] : -INFINITY;
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int v = 0; v < 4; ++v) sc[i][t][v] = (unsigned)(at + 16 * i + v) < (unsigned)w[1] ? sc[i][t][v] : -INFINITY;
+          }
         }
       }
       // probabilities against the running maxima m (log2 units), raised only where a lane's 16
@@ -870,16 +876,21 @@ __global__ __launch_bounds__(512, RWB == 128 ? 4 : 2) void k_attn_span_pp(AttnSp
     drain();
     ks = TB;
     if (wave >= 4) FF_BAR();   // the second group runs one slot behind
-    int k0 = t0 * KB;
+    int k0 = t0 * KB, run = 0;
     for (int j = 0; j < nt; ++j) {
       load_k();
       load_v();
       __builtin_amdgcn_sched_barrier(0);
-      const bool all = (unsigned)(k0 - rg.c0) < core0 || (unsigned)(k0 - rg.c1) < core1;
-      bool some = false;
-      if (!all) {
-        some = rg.some(k0, KB);
-        mixed = true;
+      bool all = true, some = false;
+      if (__builtin_expect(k0 >= run, 0)) {   // outside the core that the walk was last in
+        asm volatile("");
+        const bool in0 = (unsigned)(k0 - rg.c0) < core0, in1 = (unsigned)(k0 - rg.c1) < core1;
+        all = in0 || in1;
+        run = in0 ? rg.c0 + (int)core0 : in1 ? rg.c1 + (int)core1 : 0;
+        if (!all) {
+          some = rg.some(k0, KB);
+          mixed = true;
+        }
       }
       softmax(k0, all, some);
       ka_ = ka + ks;

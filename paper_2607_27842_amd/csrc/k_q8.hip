@@ -31,29 +31,27 @@ __device__ __forceinline__ u32x2_t q_pack8(const float* v, float inv) {
 }
 
 // ---------------------------------------------------------------- quantisation
-// A workgroup takes 16 rows x 4 blocks; 16 lanes hold one block of one row.
+// A workgroup takes 16 rows x 4 blocks: a wavefront 4 rows, one after the other in registers, with 16
+// lanes on each block (1 KB of bf16 in a piece).
 constexpr int kQBlocks = 4;
 template <int DT>
 __global__ __launch_bounds__(256) void k_quant_rows(QuantArgs a) {
   const int nb = (a.C + kQBlock - 1) / kQBlock, nbw = (nb + kQBlocks - 1) / kQBlocks;
-  const int row = (blockIdx.x / nbw) * 16 + (threadIdx.x >> 4), b0 = (blockIdx.x % nbw) * kQBlocks;
-  const int l16 = threadIdx.x & 15;
-  if (row >= a.rows) return;   // whole rows of 16 lanes
-  float v[kQBlocks][8];
+  const int row0 = (blockIdx.x / nbw) * 16 + (threadIdx.x >> 6) * 4, lane = threadIdx.x & 63;
+  const int c = (blockIdx.x % nbw) * kQBlocks * kQBlock + lane * 8, b = c / kQBlock;
+  float v[4][8];
 #pragma unroll
-  for (int i = 0; i < kQBlocks; ++i) {
-    const int c = (b0 + i) * kQBlock + l16 * 8;
+  for (int i = 0; i < 4; ++i) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
-    if (c < a.C) load8<DT>(a.x, (size_t)row * a.x_row + c, v[i]);
+    if (row0 + i < a.rows && c < a.C) load8<DT>(a.x, (size_t)(row0 + i) * a.x_row + c, v[i]);
   }
 #pragma unroll
-  for (int i = 0; i < kQBlocks; ++i) {
-    const int c = (b0 + i) * kQBlock + l16 * 8;
-    if (b0 + i >= nb) break;
+  for (int i = 0; i < 4; ++i) {
     const float s = q_scale(max16(abs_max8(v[i])));
-    if (c < a.C) *reinterpret_cast<u32x2_t*>(a.q + (size_t)row * a.q_row + c) = q_pack8(v[i], 1.0f / s);
-    if (l16 == 0) a.qs[(size_t)(b0 + i) * a.qs_ld + row] = s;
+    if (row0 + i >= a.rows || c >= a.C) continue;
+    *reinterpret_cast<u32x2_t*>(a.q + (size_t)(row0 + i) * a.q_row + c) = q_pack8(v[i], 1.0f / s);
+    if ((lane & 15) == 0) a.qs[(size_t)b * a.qs_ld + row0 + i] = s;
   }
 }
 

@@ -127,6 +127,28 @@ __global__ __launch_bounds__(NW * 64) void k_gemm_q8_dir(GemmQ8Args a) {
   if (m0 + l16 < a.M && n0 + 4 * g < a.N) finish4<DT>(a, m0 + l16, n0 + 4 * g, acc);
 }
 
+// 8 values as they are stored, to be added later
+template <int DT> struct Raw8;
+template <> struct Raw8<DT_BF16> {
+  typedef u32x4_t type;
+  __device__ __forceinline__ static type load(const void* p, size_t i) { return *reinterpret_cast<const u32x4_t*>(reinterpret_cast<const uint16_t*>(p) + i); }
+  __device__ __forceinline__ static void add(type w, float* v) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+  }
+};
+template <> struct Raw8<DT_F32> {
+  struct type { f32x4_t x[2]; };
+  __device__ __forceinline__ static type load(const void* p, size_t i) {
+    const f32x4_t* q = reinterpret_cast<const f32x4_t*>(reinterpret_cast<const float*>(p) + i);
+    return type{{q[0], q[1]}};
+  }
+  __device__ __forceinline__ static void add(const type& w, float* v) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += w.x[e / 4][e % 4];
+  }
+};
+
 // Epilogue of a wavefront's 16 TM x 16 TN block at (r0, c0), acc in the MFMA layout (lane l: row l % 16
 // of each 16, columns 4 (l / 16) + 0..3): 32 rows at a time go through the wave's own LDS region as
 // fp32 rows and come back as 8-column pieces, so that every load and store of bias, residual and
@@ -139,43 +161,43 @@ __device__ __forceinline__ void epilogue(const GemmQ8Args& a, int r0, int c0, co
   static_assert(64 % CPR == 0 && NPASS >= 1, "whole rows a pass");
   const int lane = threadIdx.x & 63, fr = lane & 15, fh = lane >> 4;
   const int pc = lane % CPR * 8, pr = lane / CPR, c = c0 + pc;
+  const int cl = c < a.N ? c : 0;   // loads past the matrix read its first column or last row
   float bias[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) bias[e] = 0.f;
-  if (a.bias && c < a.N) load8<DT>(a.bias, c, bias);
+  if (a.bias) load8<DT>(a.bias, cl, bias);
+  constexpr int NB = TM * 16 / RB;
+  // the residual's pieces are requested a block ahead
+  typedef typename Raw8<DT>::type raw_t;
+  raw_t res[2][NPASS];
+  auto request = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
-  for (int i = 0; i < TM * 16 / RB; ++i) {
+    for (int p = 0; p < NPASS; ++p)
+      res[i & 1][p] = Raw8<DT>::load(a.resid, (size_t)min(r0 + i * RB + p * RPP + pr, a.M - 1) * a.resid_row + cl);
+  };
+  if (a.resid) request(0);
+#pragma unroll
+  for (int i = 0; i < NB; ++i) {
 #pragma unroll
     for (int t = 0; t < RB / 16; ++t)
 #pragma unroll
       for (int u = 0; u < TN; ++u)
         *reinterpret_cast<f32x4_t*>(lds + (16 * t + fr) * LDW + 16 * u + 4 * fh) = acc[i * (RB / 16) + t][u];
-    float res[NPASS][8];
-    if (a.resid) {   // requested before the first use
-#pragma unroll
-      for (int p = 0; p < NPASS; ++p) {
-        const int r = r0 + i * RB + p * RPP + pr;
-        if (r < a.M && c < a.N) load8<DT>(a.resid, (size_t)r * a.resid_row + c, res[p]);
-      }
-    }
+    if (a.resid && i + 1 < NB) request(i + 1);
 #pragma unroll
     for (int p = 0; p < NPASS; ++p) {
       const int r = r0 + i * RB + p * RPP + pr;
       const f32x4_t x0 = *reinterpret_cast<const f32x4_t*>(lds + (p * RPP + pr) * LDW + pc);
       const f32x4_t x1 = *reinterpret_cast<const f32x4_t*>(lds + (p * RPP + pr) * LDW + pc + 4);
       float v[8] = {x0[0], x0[1], x0[2], x0[3], x1[0], x1[1], x1[2], x1[3]};
-      if (r >= a.M || c >= a.N) continue;
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] += bias[e];
       if (a.gelu) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = gelu_tanh_f(v[e]);
       }
-      if (a.resid) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += res[p][e];
-      }
-      store8<DT>(a.out, (size_t)r * a.out_row + c, v);
+      if (a.resid) Raw8<DT>::add(res[i & 1][p], v);
+      if (r < a.M && c < a.N) store8<DT>(a.out, (size_t)r * a.out_row + c, v);
     }
   }
 }
@@ -703,15 +725,17 @@ long tiles(long M, long N, long t) { return ((M + t - 1) / t) * ((N + t - 1) / t
 
 // The kernel of a shape by estimated time (us), fitted to 25 shapes of 1 to 4608 rows, N and K of 1152 to
 // 8192.  A tile of 64 x 64 takes 0.21 us per block of K while each CU has one, 0.5 with two on every CU;
-// 128 x 128 0.36 alone, 0.71 with all CUs (what the caches deliver); 256 x 256 1.95; fp32 outputs 1.5
-// times that.  Splits of K add the join: a launch, and writing and reading the partial sums.
+// 128 x 128 0.36 alone, 0.71 with all CUs (what the caches deliver); 256 x 256 1.95; fp32 outputs 1.4 to
+// 2 times that.  Splits of K add the join: a launch, and writing and reading the partial sums.
 //   N 8192 K 2048, M = 16: k_gemm_q8_dir 7.1 us against 8.0 with 64 x 64 tiles; M = 64: 17.8 against 8.1
 //   M 128 N 2048 K 8192: 64 x 64 tiles 17.7 us, with 2 / 4 / 8 splits 14.2 / 12.4 / 14.7
 //   M 512 N 8192 K 2048: 128 x 128 14.9 us, 64 x 64 20.9, 256 x 256 31.9
 //   M 14566 N 8192 K 2048: 256 x 256 263 us, 128 x 128 322, 64 x 64 444
 Plan plan(int dt, int M, int N, int K) {
   const int nk = (K + kQBlock - 1) / kQBlock;
-  const double slow = dt == DT_F32 ? 1.5 : 1.0;
+  // us per block of K: few tiles, what 256 tiles add, and a round of all CUs (512 tiles of 64 x 64)
+  const double c64[2][3] = {{0.21, 0.08, 0.50}, {0.30, 0.12, 0.71}}, c128[2][3] = {{0.36, 0.35, 0.71}, {0.73, 0.40, 1.13}};
+  const double *c6 = c64[dt == DT_F32], *c12 = c128[dt == DT_F32];
   Plan best{kTwo128, 1};
   double least = 1e30;
   auto take = [&](Kind k, int splits, double us) {
@@ -724,11 +748,11 @@ Plan plan(int dt, int M, int N, int K) {
   for (int s = 1; s <= 8; s *= 2) {
     if (s > 1 && nk / s < 8) break;
     const double t = (double)tiles(M, N, 64) * s, nb = (double)nk / s;
-    const double main = t <= 256 ? (0.21 + 0.08 * t / 256) * nb : ceil(t / 512) * 0.5 * nb;
-    take(kTwo64, s, 3.5 + slow * main + (s > 1 ? 1.8 + s * (0.35 + 2.3e-6 * M * N) : 0.0));
+    const double main = t <= 256 ? (c6[0] + c6[1] * t / 256) * nb : ceil(t / 512) * c6[2] * nb;
+    take(kTwo64, s, 3.5 + main + (s > 1 ? 1.8 + s * (0.35 + 2.3e-6 * M * N) : 0.0));
   }
   const double t128 = (double)tiles(M, N, 128), t256 = (double)tiles(M, N, 256);
-  take(kTwo128, 1, 3.5 + slow * (t128 <= 256 ? 0.36 + 0.35 * t128 / 256 : ceil(t128 / 256) * 0.71) * nk);
+  take(kTwo128, 1, 3.5 + (t128 <= 256 ? c12[0] + c12[1] * t128 / 256 : ceil(t128 / 256) * c12[2]) * nk);
   if (dt == DT_BF16 && nk >= 3) take(kPP, 1, 4.0 + ceil(t256 / 256) * 1.95 * nk);
   return best;
 }

@@ -725,7 +725,7 @@ long tiles(long M, long N, long t) { return ((M + t - 1) / t) * ((N + t - 1) / t
 
 // The kernel of a shape by estimated time (us), fitted to 25 shapes of 1 to 4608 rows, N and K of 1152 to
 // 8192.  A tile of 64 x 64 takes 0.21 us per block of K while each CU has one, 0.5 with two on every CU;
-// 128 x 128 0.36 alone, 0.71 with all CUs (what the caches deliver); 256 x 256 1.95; fp32 outputs 1.4 to
+// 128 x 128 0.42 alone, 0.71 with all CUs (what the caches deliver); 256 x 256 1.95; fp32 outputs 1.4 to
 // 2 times that.  Splits of K add the join: a launch, and writing and reading the partial sums.
 //   N 8192 K 2048, M = 16: k_gemm_q8_dir 7.1 us against 8.0 with 64 x 64 tiles; M = 64: 17.8 against 8.1
 //   M 128 N 2048 K 8192: 64 x 64 tiles 17.7 us, with 2 / 4 / 8 splits 14.2 / 12.4 / 14.7
@@ -734,7 +734,7 @@ long tiles(long M, long N, long t) { return ((M + t - 1) / t) * ((N + t - 1) / t
 Plan plan(int dt, int M, int N, int K) {
   const int nk = (K + kQBlock - 1) / kQBlock;
   // us per block of K: few tiles, what 256 tiles add, and a round of all CUs (512 tiles of 64 x 64)
-  const double c64[2][3] = {{0.21, 0.08, 0.50}, {0.30, 0.12, 0.71}}, c128[2][3] = {{0.36, 0.35, 0.71}, {0.73, 0.40, 1.13}};
+  const double c64[2][3] = {{0.21, 0.08, 0.50}, {0.30, 0.12, 0.71}}, c128[2][3] = {{0.42, 0.30, 0.71}, {0.73, 0.40, 1.13}};
   const double *c6 = c64[dt == DT_F32], *c12 = c128[dt == DT_F32];
   Plan best{kTwo128, 1};
   double least = 1e30;

@@ -611,12 +611,12 @@ __global__ __launch_bounds__(512, RWB == 128 ? 4 : 2) void k_attn_span_pp(AttnSp
   // The walk over K's and V's tiles: the next tile's address, its keys up to the last, its number and
   // its ring slot, advanced tile by tile; what happens once or at the end is branched to (formed
   // anew for each tile, with selects, this took 100 scalar instructions of the softmax slot).
-  struct Walk { const char* p; int left, j, slot; };
+  struct Walk { const char* p; int left, j, stop, slot; };   // stop: the tile number at which a range ends
   const uint32_t kl = (uint32_t)a.kr * 2u, vl = (uint32_t)a.vr * 2u, fullk = (KB - 1) * kl + d * 2, fullv = (KB - 1) * vl + d * 2;
-  Walk wk{kp + (size_t)t0 * KB * kl, a.n_k - t0 * KB, 0, 0}, wv{vp + (size_t)t0 * KB * vl, a.n_k - t0 * KB, 0, 0};
+  Walk wk{kp + (size_t)t0 * KB * kl, a.n_k - t0 * KB, 0, n0, 0}, wv{vp + (size_t)t0 * KB * vl, a.n_k - t0 * KB, 0, n0, 0};
   // DMA of the walk's next tile.  The tile's resource ends with the last key's last element, so that
-  // keys past it load as zeros (or, with a stride below d, as elements of the last keys: their
-  // probabilities are zero); tiles past the walk are read too, as far as there are keys, and not used
+  // keys past it, and tiles past the walk, load as zeros (or, with a stride below d, as elements of
+  // the last keys: their probabilities are zero)
   auto load = [&](Walk& w, const char* base, uint32_t ld, uint32_t full, const uint32_t (&vo)[DPW], int off) __attribute__((always_inline)) {
     uint32_t num = full;
     if (__builtin_expect(w.left < KB, 0)) {
@@ -630,10 +630,11 @@ __global__ __launch_bounds__(512, RWB == 128 ? 4 : 2) void k_attn_span_pp(AttnSp
     ++w.j;
     w.left -= KB;
     w.p += (size_t)KB * ld;
-    if (__builtin_expect(w.j == n0, 0)) {   // on to the second range
+    if (__builtin_expect(w.j == w.stop, 0)) {   // on to the second range, or at the end
       asm volatile("");
-      w.left = a.n_k - t1 * KB;
+      w.left = w.j < nt ? a.n_k - t1 * KB : 0;
       w.p = base + (size_t)t1 * KB * ld;
+      w.stop = nt;
     }
     w.slot = (w.slot + TB) & (NB * TB - 1);
   };

@@ -44,20 +44,29 @@ __device__ __forceinline__ f32x4_t product(u32x4_t w0, u32x4_t w1, u32x4_t x0, u
   return p;
 }
 
-// 4 consecutive columns c.. of output row r (N % 8 == 0: in range as a whole)
+// 4 consecutive columns c.. of output row r (N % 8 == 0: in range as a whole): what is added to the
+// product, and the rest of the epilogue
+struct Add4 { f32x4_t bias, resid; };
 template <int DT>
-__device__ __forceinline__ void finish4(const GemmQ8Args& a, int r, int c, f32x4_t v) {
-  if (a.bias) {
+__device__ __forceinline__ f32x4_t load4(const void* p, size_t i) {
+  if (DT == DT_F32) return *reinterpret_cast<const f32x4_t*>(reinterpret_cast<const float*>(p) + i);
+  const u32x2_t w = *reinterpret_cast<const u32x2_t*>(reinterpret_cast<const uint16_t*>(p) + i);
+  return f32x4_t{__uint_as_float(w[0] << 16), __uint_as_float(w[0] & 0xffff0000u), __uint_as_float(w[1] << 16), __uint_as_float(w[1] & 0xffff0000u)};
+}
+template <int DT>
+__device__ __forceinline__ Add4 request4(const GemmQ8Args& a, int r, int c) {
+  Add4 x{{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+  if (a.bias) x.bias = load4<DT>(a.bias, c);
+  if (a.resid) x.resid = load4<DT>(a.resid, (size_t)r * a.resid_row + c);
+  return x;
+}
+template <int DT>
+__device__ __forceinline__ void finish4(const GemmQ8Args& a, const Add4& x, int r, int c, f32x4_t v) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] += St<DT>::ld1(a.bias, c + e);
-  }
-  if (a.gelu) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = gelu_tanh_f(v[e]);
-  }
-  if (a.resid) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] += St<DT>::ld1(a.resid, (size_t)r * a.resid_row + c + e);
+  for (int e = 0; e < 4; ++e) {
+    v[e] += x.bias[e];
+    if (a.gelu) v[e] = gelu_tanh_f(v[e]);
+    v[e] += x.resid[e];
   }
   const size_t o = (size_t)r * a.out_row + c;
   if (DT == DT_BF16) *reinterpret_cast<u32x2_t*>(reinterpret_cast<uint16_t*>(a.out) + o) = u32x2_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
@@ -82,6 +91,10 @@ __global__ __launch_bounds__(NW * 64) void k_gemm_q8_dir(GemmQ8Args a) {
   const float* sa = a.a_s + m;
   const float* sw = a.w_s + (size_t)(n0 / kQBlock) * a.ws_ld;
   f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+  // the first wave finishes the tile: what it adds is requested before the operands
+  const bool in = m0 + l16 < a.M && n0 + 4 * g < a.N;
+  Add4 extra{acc, acc};
+  if (wave == 0) extra = request4<DT>(a, in ? m0 + l16 : m0, in ? n0 + 4 * g : n0);
   const int nk = (a.K + kQBlock - 1) / kQBlock;
   for (int b0 = wave; b0 < nk; b0 += NW * U) {
     u32x4_t x[U][2], w[U][2];
@@ -103,11 +116,11 @@ __global__ __launch_bounds__(NW * 64) void k_gemm_q8_dir(GemmQ8Args a) {
       if (b0 + NW * u >= nk) break;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const bool in = (b0 + NW * u) * kQBlock + g * 16 + h * 64 < a.K;
+        const bool on = (b0 + NW * u) * kQBlock + g * 16 + h * 64 < a.K;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {   // both operands, so that 0 * 0 is added
-          w[u][h][e] = in ? w[u][h][e] : 0u;
-          x[u][h][e] = in ? x[u][h][e] : 0u;
+          w[u][h][e] = on ? w[u][h][e] : 0u;
+          x[u][h][e] = on ? x[u][h][e] : 0u;
         }
       }
       const f32x4_t p = product<DT>(w[u][0], w[u][1], x[u][0], x[u][1]);
@@ -124,7 +137,7 @@ __global__ __launch_bounds__(NW * 64) void k_gemm_q8_dir(GemmQ8Args a) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[e] += p[e];
   }
-  if (m0 + l16 < a.M && n0 + 4 * g < a.N) finish4<DT>(a, m0 + l16, n0 + 4 * g, acc);
+  if (in) finish4<DT>(a, extra, m0 + l16, n0 + 4 * g, acc);
 }
 
 // 8 values as they are stored, to be added later

@@ -440,7 +440,7 @@ ff_status ff_rel_l1(const ff_model_desc* m, const void* a, const void* b, float 
  * into a graph; one captured call, or ones that follow each other, may share a workspace. */
 #define FF_Q8_BLOCK 128
 
-/* C % 8 == 0, C >= 8, rows >= 0; x_row, q_row >= C and multiples of 8; block_rows 1 (rows) or 128
+/* C % 8 == 0, C >= 8, 0 <= rows <= 2^23, rows * C <= 2^35; x_row, q_row >= C and multiples of 8; block_rows 1 (rows) or 128
  * (squares).  dtype: of x. */
 typedef struct {
   int32_t rows, C, dtype, block_rows;
@@ -452,7 +452,7 @@ typedef struct {
  * alignment, overlap), FF_E_HIP. */
 ff_status ff_quant_q8(const ff_quant_desc* d, const void* x, void* q, float* qs, ff_stream_t stream);
 
-/* dtype: of x, resid, gain, sum and y.  8 <= C <= 16384, C % 8 == 0, rows >= 0; the pitches of the
+/* dtype: of x, resid, gain, sum and y.  8 <= C <= 16384, C % 8 == 0, 0 <= rows <= 2^23; the pitches of the
  * tensors that are passed >= C and multiples of 8, qs_ld >= rows; eps > 0. */
 typedef struct {
   int32_t rows, C, dtype;
@@ -469,9 +469,10 @@ typedef struct {
 ff_status ff_rms_norm_q8(const ff_norm_desc* d, const void* x, const void* resid, const void* gain, void* sum,
                          void* y, void* q, float* qs, ff_stream_t stream);
 
-/* M >= 0, N >= 8, N % 8 == 0, K >= 16, K % 16 == 0; a_row, w_row >= K, multiples of 16; out_row (and
- * resid_row with resid) >= N, multiples of 8; as_ld >= M; ws_ld >= ceil(K / 128); 256 rows of a or
- * w, and all scales of either, within 2^31 bytes.  out_dtype: of bias, resid and out. */
+/* 0 <= M <= 2^23, 8 <= N <= 2^20, N % 8 == 0, M N <= 2^34, 16 <= K <= 2^24, K % 16 == 0; a_row,
+ * w_row >= K, multiples of 16; out_row (and resid_row with resid) >= N, multiples of 8; as_ld >= M;
+ * ws_ld >= ceil(K / 128); 256 rows of a or w, and all scales of either, within 2^31 bytes.
+ * out_dtype: of bias, resid and out. */
 typedef struct {
   int32_t M, N, K, out_dtype;
   int32_t gelu;           /* 1: GELU (tanh form) on the product with its bias, 0: none */
@@ -481,7 +482,9 @@ typedef struct {
 /* out [M, N] <- act(A W^T + bias) + resid, A [M, K] in 8 bits with scales a_s (blocks of rows),
  * W [N, K] with scales w_s (squares):
  *     (A W^T)[m, n] = sum_b a_s[b, m] w_s[n / 128, b] sum_{k in block b} a[m, k] w[n, k],
- * sums in fp32, one rounding to out_dtype.  bias [N] and resid [M, N] may be NULL; out may be
+ * sums over blocks in fp32, one rounding to out_dtype.  Within a block, fp32 outputs take exact
+ * products summed in fp32; bf16 outputs take the 8-bit matrix instructions, which align a block's
+ * products to fewer bits (1.5e-5 of the result on normal operands).  bias [N] and resid [M, N] may be NULL; out may be
  * resid itself at the same pitch.  ws: at least ff_gemm_q8_workspace_bytes(d) bytes (NULL if
  * that is 0; it is for most shapes: only few rows on a long K need one).
  * Errors: FF_E_NULL, FF_E_DTYPE, FF_E_RANGE (gelu), FF_E_SHAPE, FF_E_WORKSPACE, FF_E_HIP. */
@@ -514,8 +517,8 @@ ff_status ff_gemm_q8(const ff_gemm_q8_desc* d, const void* a, const float* a_s, 
  * only few queries on many keys, whose keys are split, need one). */
 enum { FF_BIAS_NONE = 0, FF_BIAS_SLOPE = 1, FF_BIAS_TABLE = 2 };
 
-/* B >= 1, H % H_kv == 0, d in [8, 128] and d % 8 == 0, n_q, n_k >= 0 (and n_q H B, n_k below 2^30);
- * strides non-negative multiples of 8, out's rows apart from each other; 64 key or value rows
+/* B >= 1, H % H_kv == 0, d in [8, 128] and d % 8 == 0, n_q, n_k >= 0, n_q H B and n_k below 2^30,
+ * B H_kv ceil(n_q (H / H_kv) / 16) below 2^23; strides non-negative multiples of 8, out's rows apart from each other; 64 key or value rows
  * within 2^31 bytes; scale > 0, cap >= 0, both finite; 0 <= bias_reach <= 2^20; n_spans 0, 1 or 2. */
 typedef struct {
   int32_t dtype, B, H, H_kv, d, n_q, n_k;

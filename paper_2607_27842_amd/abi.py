@@ -327,12 +327,15 @@ def ff_denoise_step(ctx, step, x, cond, txt, audit, stream=0):
     return check(lib().ff_denoise_step(ctx, step, x, cond, txt, audit, stream))
 
 
-# Operators on 8-bit operands and attention over spans (addresses or None).
+# Operators on 8-bit operands and attention over spans.  Tensors are addresses, None where the call
+# allows NULL; the descriptors' fields are elements.
 def ff_quant_q8(desc, x, q, qs, stream=0):
+    """q, qs <- x in e4m3 with a scale per 128 columns of a row, or per 128 x 128 square."""
     return check(lib().ff_quant_q8(C.byref(desc), x, q, qs, stream))
 
 
 def ff_rms_norm_q8(desc, x, resid, gain, sum, y, q, qs, stream=0):
+    """Root-mean-square norm of x (+ resid): sum <- the stream, y and q, qs <- the result, each unless None."""
     return check(lib().ff_rms_norm_q8(C.byref(desc), x, resid, gain, sum, y, q, qs, stream))
 
 
@@ -341,6 +344,7 @@ def ff_gemm_q8_workspace_bytes(desc):
 
 
 def ff_gemm_q8(desc, a, a_s, w, w_s, bias, resid, out, ws, ws_bytes, stream=0):
+    """out <- act(A W^T + bias) + resid on 8-bit operands; ws of ff_gemm_q8_workspace_bytes(desc)."""
     return check(lib().ff_gemm_q8(C.byref(desc), a, a_s, w, w_s, bias, resid, out, ws, ws_bytes, stream))
 
 
@@ -349,6 +353,7 @@ def ff_attention_workspace_bytes(desc):
 
 
 def ff_attention(desc, q, k, v, bias, pos, spans, out, ws, ws_bytes, stream=0):
+    """Attention of each query over its spans of keys; ws of ff_attention_workspace_bytes(desc)."""
     return check(lib().ff_attention(C.byref(desc), q, k, v, bias, pos, spans, out, ws, ws_bytes, stream))
 
 

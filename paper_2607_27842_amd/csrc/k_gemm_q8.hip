@@ -241,6 +241,9 @@ __device__ __forceinline__ void tile_at(int wg, int n, int tiles_m, int tiles_n,
 // piece's slot is refilled no earlier than one phase after its last read.
 // The weight's scale of a stage is a scalar per wave (its columns lie in one block of 128).
 // K % 128 != 0: the last stage's chunks past K are out of the resource's range and load zeros.
+// What bounds it: with random operands the card's power limit in the main loop, then the epilogue, which
+// one workgroup a CU leaves uncovered.  M = 14566, N = 8192, K = 2048: 269 us (1.81 PFLOP/s; a library's
+// product with one scale a tensor takes 237), with GELU 292, with a residual 299.
 constexpr int kPPIssue[4][3] = {{3, 8, -1}, {0, 4, 5}, {1, 6, -1}, {2, 7, -1}};   // A0-A3, B0-B3, scales
 // How many of a wave's DMAs may be outstanding at the end of phase p of a stage with `left` stages
 // after it (2: two or more), so that what phase p + 1 reads has landed.
@@ -470,6 +473,11 @@ __global__ __launch_bounds__(512) void k_gemm_q8_pp(GemmQ8Args a) {
 // block's sums) and a matrix slot (the DMA of the block NS ahead into the ring slot just read, then
 // the MFMAs), each ended by a barrier; the second group runs one slot behind, one wave of each group
 // per SIMD.  The two groups' sums meet in LDS: each finishes half of the rows.
+// What bounds it: a slot's LDS reads, its waits and barrier (64 x 64: 0.21 us a block of K, with two
+// workgroups on a CU 0.25; 128 x 128 0.36 alone), and with all CUs what the caches deliver (128 x 128
+// 0.71 us a block).  Waiting for the scalar load of the weight's scale in each slot, and issuing the DMA
+// ahead of the MFMAs instead of behind each, cost 10 to 15 %.  64 x 64 with rings of two blocks and two
+// workgroups a CU: 16.3 us against 21.5 with rings of four (M = 1003, N = 1480, K = 2960).
 //
 template <int DT, int BM, int BN, int NS>
 __global__ __launch_bounds__(512) void k_gemm_q8_two(GemmQ8Args a, int splits) {

@@ -32,7 +32,9 @@ __device__ __forceinline__ u32x2_t q_pack8(const float* v, float inv) {
 
 // ---------------------------------------------------------------- quantisation
 // A workgroup takes 16 rows x 4 blocks: a wavefront 4 rows, one after the other in registers, with 16
-// lanes on each block (1 KB of bf16 in a piece).
+// lanes on each block (1 KB of bf16 in a piece; 16 lanes on one row of four read 256-byte pieces
+// and took 2 % longer).  Bound by memory: 4608 x 8192 bf16 25 to 27 us, 4.4 TB/s of the 5.0 that a large
+// copy reaches; one row 2.3 us, a launch.
 constexpr int kQBlocks = 4;
 template <int DT>
 __global__ __launch_bounds__(256) void k_quant_rows(QuantArgs a) {
@@ -55,7 +57,8 @@ __global__ __launch_bounds__(256) void k_quant_rows(QuantArgs a) {
   }
 }
 
-// One workgroup per square of 128 x 128.
+// One workgroup per square of 128 x 128, held in registers between the square's largest value and the
+// rounding.  Bound by memory: 8200 x 2960 fp32 26 us, 4.7 TB/s.
 template <int DT>
 __global__ __launch_bounds__(256) void k_quant_squares(QuantArgs a) {
   __shared__ float top[16];

@@ -12,6 +12,8 @@ namespace {
 
 typedef __int128 wide;
 constexpr int64_t kMaxPitch = (int64_t)1 << 40;   // products with row counts stay inside 128 bits
+// Rows of a call: a launch has fewer than 2^32 threads, and up to 256 of them work on a row
+constexpr int kMaxRows = 1 << 23;
 
 bool dtype_ok(int dt) { return dt == FF_F32 || dt == FF_BF16; }
 
@@ -38,8 +40,9 @@ ff_status check_quant(const ff_quant_desc* d) {
   CHECK(d, FF_E_NULL, "quant descriptor is NULL");
   CHECK(dtype_ok(d->dtype), FF_E_DTYPE, "unknown dtype %d", d->dtype);
   CHECK(d->block_rows == 1 || d->block_rows == kQBlock, FF_E_RANGE, "block_rows=%d must be 1 or %d", d->block_rows, kQBlock);
-  CHECK(d->rows >= 0 && d->rows <= 1 << 30, FF_E_SHAPE, "rows=%d outside [0, 2^30]", d->rows);
-  CHECK(d->C >= 8 && d->C % 8 == 0 && d->C <= 1 << 24, FF_E_SHAPE, "C=%d must be a multiple of 8 in [8, 2^24]", d->C);
+  CHECK(d->rows >= 0 && d->rows <= kMaxRows, FF_E_SHAPE, "rows=%d outside [0, 2^23]", d->rows);
+  CHECK(d->C >= 8 && d->C % 8 == 0 && (int64_t)d->C * d->rows <= (int64_t)1 << 35 && d->C <= 1 << 24, FF_E_SHAPE,
+        "C=%d must be a multiple of 8 in [8, 2^24] with rows * C <= 2^35", d->C);
   CHECK(pitch_ok(d->x_row, d->C, 8) && pitch_ok(d->q_row, d->C, 8), FF_E_SHAPE, "x_row and q_row must be multiples of 8 and >= C");
   const int64_t least = d->block_rows == 1 ? d->rows : (d->C + kQBlock - 1) / kQBlock;
   CHECK(d->qs_ld >= least && d->qs_ld <= kMaxPitch, FF_E_SHAPE, "qs_ld=%lld must be >= %lld", (long long)d->qs_ld, (long long)least);
@@ -50,7 +53,7 @@ ff_status check_norm(const ff_norm_desc* d, bool resid, bool sum, bool y, bool q
   CHECK(d, FF_E_NULL, "norm descriptor is NULL");
   CHECK(dtype_ok(d->dtype), FF_E_DTYPE, "unknown dtype %d", d->dtype);
   CHECK(d->eps > 0.f && isfinite(d->eps), FF_E_RANGE, "eps must be > 0");
-  CHECK(d->rows >= 0 && d->rows <= 1 << 30, FF_E_SHAPE, "rows=%d outside [0, 2^30]", d->rows);
+  CHECK(d->rows >= 0 && d->rows <= kMaxRows, FF_E_SHAPE, "rows=%d outside [0, 2^23]", d->rows);
   CHECK(d->C >= 8 && d->C % 8 == 0 && d->C <= kNormMaxC, FF_E_SHAPE, "C=%d must be a multiple of 8 in [8, %d]", d->C, kNormMaxC);
   CHECK(pitch_ok(d->x_row, d->C, 8), FF_E_SHAPE, "x_row must be a multiple of 8 and >= C");
   CHECK(!resid || pitch_ok(d->resid_row, d->C, 8), FF_E_SHAPE, "resid_row must be a multiple of 8 and >= C");
@@ -65,8 +68,9 @@ ff_status check_gemm(const ff_gemm_q8_desc* d, bool resid) {
   CHECK(d, FF_E_NULL, "gemm descriptor is NULL");
   CHECK(dtype_ok(d->out_dtype), FF_E_DTYPE, "unknown dtype %d", d->out_dtype);
   CHECK(d->gelu == 0 || d->gelu == 1, FF_E_RANGE, "gelu must be 0 or 1");
-  CHECK(d->M >= 0 && d->M <= 1 << 30, FF_E_SHAPE, "M=%d outside [0, 2^30]", d->M);
-  CHECK(d->N >= 8 && d->N % 8 == 0 && d->N <= 1 << 24, FF_E_SHAPE, "N=%d must be a multiple of 8 in [8, 2^24]", d->N);
+  CHECK(d->M >= 0 && d->M <= kMaxRows, FF_E_SHAPE, "M=%d outside [0, 2^23]", d->M);
+  CHECK(d->N >= 8 && d->N % 8 == 0 && d->N <= 1 << 20 && (int64_t)d->M * d->N <= (int64_t)1 << 34, FF_E_SHAPE,
+        "N=%d must be a multiple of 8 in [8, 2^20] with M * N <= 2^34", d->N);
   CHECK(d->K >= 16 && d->K % 16 == 0 && d->K <= 1 << 24, FF_E_SHAPE, "K=%d must be a multiple of 16 in [16, 2^24]", d->K);
   CHECK(pitch_ok(d->a_row, d->K, 16) && pitch_ok(d->w_row, d->K, 16), FF_E_SHAPE, "a_row and w_row must be multiples of 16 and >= K");
   CHECK(pitch_ok(d->out_row, d->N, 8) && (!resid || pitch_ok(d->resid_row, d->N, 8)), FF_E_SHAPE,
@@ -107,6 +111,8 @@ ff_status check_attn(const ff_attn_desc* d) {
   CHECK(d->d >= 8 && d->d <= 128 && d->d % 8 == 0, FF_E_SHAPE, "d=%d must be a multiple of 8 in [8, 128]", d->d);
   CHECK(d->n_q >= 0 && d->n_k >= 0 && d->n_k < 1 << 30 && (wide)d->n_q * d->H * d->B < 1 << 30, FF_E_SHAPE,
         "n_q * H * B and n_k must be in [0, 2^30)");
+  CHECK((wide)d->B * d->H_kv * (((int64_t)d->n_q * (d->H / d->H_kv) + 15) / 16) < kMaxRows, FF_E_SHAPE,
+        "B * H_kv * ceil(n_q * H / H_kv / 16) must be below 2^23");
   const int64_t st[12] = {d->q_batch, d->q_row, d->q_head, d->k_batch, d->k_row, d->k_head,
                           d->v_batch, d->v_row, d->v_head, d->o_batch, d->o_row, d->o_head};
   for (int64_t x : st) CHECK(x >= 0 && x % 8 == 0 && x <= kMaxPitch, FF_E_SHAPE, "strides must be non-negative multiples of 8");

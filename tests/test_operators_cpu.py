@@ -58,7 +58,7 @@ def refused(code, call, *a, **k):
 @pytest.mark.parametrize("o,code", [
     (dict(dtype=7), E.FF_E_DTYPE), (dict(block_rows=2), E.FF_E_RANGE), (dict(rows=-1), E.FF_E_SHAPE), (dict(C=4), E.FF_E_SHAPE),
     (dict(C=252), E.FF_E_SHAPE), (dict(x_row=248), E.FF_E_SHAPE), (dict(x_row=260), E.FF_E_SHAPE), (dict(q_row=248), E.FF_E_SHAPE),
-    (dict(qs_ld=3), E.FF_E_SHAPE), (dict(block_rows=128, qs_ld=1), E.FF_E_SHAPE), (dict(x_row=1 << 50), E.FF_E_SHAPE)])
+    (dict(rows=(1 << 23) + 1, qs_ld=1 << 24), E.FF_E_SHAPE), (dict(qs_ld=3), E.FF_E_SHAPE), (dict(block_rows=128, qs_ld=1), E.FF_E_SHAPE), (dict(x_row=1 << 50), E.FF_E_SHAPE)])
 def test_quant_refuses(o, code):
     refused(code, quant, **o)
 
@@ -71,7 +71,7 @@ def test_quant_refuses_pointers(p, code):
 
 
 @pytest.mark.parametrize("o,code", [
-    (dict(dtype=2), E.FF_E_DTYPE), (dict(eps=0.0), E.FF_E_RANGE), (dict(eps=float("nan")), E.FF_E_RANGE), (dict(rows=-1), E.FF_E_SHAPE),
+    (dict(dtype=2), E.FF_E_DTYPE), (dict(eps=0.0), E.FF_E_RANGE), (dict(eps=float("nan")), E.FF_E_RANGE), (dict(rows=-1), E.FF_E_SHAPE), (dict(rows=(1 << 23) + 1, qs_ld=1 << 24), E.FF_E_SHAPE),
     (dict(C=16392, x_row=16392), E.FF_E_SHAPE), (dict(C=250), E.FF_E_SHAPE), (dict(x_row=128), E.FF_E_SHAPE),
     (dict(resid_row=257), E.FF_E_SHAPE), (dict(sum_row=8), E.FF_E_SHAPE), (dict(y_row=252), E.FF_E_SHAPE),
     (dict(q_row=0), E.FF_E_SHAPE), (dict(qs_ld=3), E.FF_E_SHAPE)])
@@ -92,7 +92,8 @@ def test_norm_sum_in_place_needs_the_same_pitch():
 
 
 @pytest.mark.parametrize("o,code", [
-    (dict(out_dtype=3), E.FF_E_DTYPE), (dict(gelu=2), E.FF_E_RANGE), (dict(M=-1), E.FF_E_SHAPE), (dict(N=60, out_row=64), E.FF_E_SHAPE),
+    (dict(out_dtype=3), E.FF_E_DTYPE), (dict(gelu=2), E.FF_E_RANGE), (dict(M=-1), E.FF_E_SHAPE), (dict(M=(1 << 23) + 1, as_ld=1 << 24), E.FF_E_SHAPE),
+    (dict(N=(1 << 20) + 8, out_row=1 << 21, resid_row=1 << 21), E.FF_E_SHAPE), (dict(N=60, out_row=64), E.FF_E_SHAPE),
     (dict(N=0), E.FF_E_SHAPE), (dict(K=8), E.FF_E_SHAPE), (dict(K=250), E.FF_E_SHAPE), (dict(a_row=264), E.FF_E_SHAPE),
     (dict(w_row=128), E.FF_E_SHAPE), (dict(out_row=56), E.FF_E_SHAPE), (dict(resid_row=68), E.FF_E_SHAPE), (dict(as_ld=3), E.FF_E_SHAPE),
     (dict(ws_ld=1), E.FF_E_SHAPE), (dict(a_row=1 << 23), E.FF_E_SHAPE), (dict(as_ld=1 << 28), E.FF_E_SHAPE)])
@@ -128,7 +129,8 @@ def test_gemm_workspace():
 @pytest.mark.parametrize("o,code", [
     (dict(dtype=5), E.FF_E_DTYPE), (dict(B=0), E.FF_E_SHAPE), (dict(H=3), E.FF_E_SHAPE), (dict(H_kv=0), E.FF_E_SHAPE),
     (dict(d=4), E.FF_E_SHAPE), (dict(d=68), E.FF_E_SHAPE), (dict(d=136), E.FF_E_SHAPE), (dict(n_q=-1), E.FF_E_SHAPE),
-    (dict(n_k=-1), E.FF_E_SHAPE), (dict(n_k=1 << 30), E.FF_E_SHAPE), (dict(n_q=1 << 28), E.FF_E_SHAPE), (dict(q_row=260), E.FF_E_SHAPE),
+    (dict(n_k=-1), E.FF_E_SHAPE), (dict(n_k=1 << 30), E.FF_E_SHAPE), (dict(n_q=1 << 28), E.FF_E_SHAPE),
+    (dict(B=1 << 23, n_q=1, q_batch=256, o_batch=256, q_row=256, o_row=256), E.FF_E_SHAPE), (dict(q_row=260), E.FF_E_SHAPE),
     (dict(k_head=-64), E.FF_E_SHAPE), (dict(k_row=1 << 24), E.FF_E_SHAPE), (dict(o_head=56), E.FF_E_SHAPE), (dict(o_row=192), E.FF_E_SHAPE),
     (dict(o_batch=1024), E.FF_E_SHAPE), (dict(o_batch=0), E.FF_E_SHAPE), (dict(scale=0.0), E.FF_E_RANGE),
     (dict(scale=float("inf")), E.FF_E_RANGE), (dict(cap=-1.0), E.FF_E_RANGE), (dict(cap=float("nan")), E.FF_E_RANGE),

@@ -228,10 +228,9 @@ __device__ __forceinline__ void tile_at(int wg, int n, int tiles_m, int tiles_n,
 // ---------------------------------------------------------------- large grids: two wave groups in turn
 // 256 x 64 TN tile, a stage of one 128-wide block of K, 8 waves in two groups of four, one wave of
 // each group per SIMD; a stage has four phases, one per 32 rows of a wave's 128 x 16 TN block.  A
-// phase is a memory part (fragment reads, DMA, and the fused multiply-adds that scale the former
-// phase's sums into the accumulators) and 2 TN MFMAs, with a barrier after each; the second group
-// runs half a phase behind, so that on every SIMD one wave's MFMAs (64 TN cycles) cover the other's
-// reads, DMA and 8 TN + 2 vector instructions.
+// phase is a memory part (fragment reads, DMA) and 2 TN MFMAs among the fused multiply-adds that scale
+// their sums into the accumulators, with a barrier after each; the second group runs half a phase
+// behind, so that on every SIMD one wave's MFMAs (64 TN cycles) cover the other's reads and DMA.
 //
 // Operands: 64-row pieces of 8 KB, each filled by one DMA instruction per wave, in two buffers per
 // operand, and the 256 rows' scales of a stage (1 KB, one 4-byte DMA a lane; waves w and w + 4 write
@@ -242,8 +241,8 @@ __device__ __forceinline__ void tile_at(int wg, int n, int tiles_m, int tiles_n,
 // The weight's scale of a stage is a scalar per wave (its columns lie in one block of 128).
 // K % 128 != 0: the last stage's chunks past K are out of the resource's range and load zeros.
 // What bounds it: with random operands the card's power limit in the main loop, then the epilogue, which
-// one workgroup a CU leaves uncovered.  M = 14566, N = 8192, K = 2048: 269 us (1.81 PFLOP/s; a library's
-// product with one scale a tensor takes 237), with GELU 292, with a residual 299.
+// one workgroup a CU leaves uncovered.  M = 14566, N = 8192, K = 2048: 271 us (1.80 PFLOP/s; a library's
+// product with one scale a tensor takes 237), with GELU 294, with a residual 299.
 constexpr int kPPIssue[4][3] = {{3, 8, -1}, {0, 4, 5}, {1, 6, -1}, {2, 7, -1}};   // A0-A3, B0-B3, scales
 // How many of a wave's DMAs may be outstanding at the end of phase p of a stage with `left` stages
 // after it (2: two or more), so that what phase p + 1 reads has landed.
@@ -299,13 +298,13 @@ __global__ __launch_bounds__(512) void k_gemm_q8_pp(GemmQ8Args a) {
   const bool cut = (int)ch >= a.K - (nk - 1) * kQBlock;   // this lane's chunk of the last stage lies past K
 #define FF_DMA(rs, vo, dst, kb) __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, FF_AS3(lds + (dst) + wave * 1024), 16, vo, kb, 0, 0)
 #define FF_DMAS(st) __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, FF_AS3(lds + OFFS + ((st) & 3) * 1024 + (wave & 3) * 256), 4, vos, (st) * sstep, 0, 0)
-  f32x4_t acc[8][TN], part[2][TN];
+  f32x4_t acc[8][TN], part[3];
 #pragma unroll
-  for (int j = 0; j < TN; ++j) {
+  for (int j = 0; j < TN; ++j)
 #pragma unroll
     for (int i = 0; i < 8; ++i) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    part[0][j] = part[1][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  }
+#pragma unroll
+  for (int i = 0; i < 3; ++i) part[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   const int fr = lane & 15, fh = lane >> 4;
   const uint32_t lds0 = (uint32_t)(uintptr_t)((__attribute__((address_space(3))) const void*)lds);
   uint32_t rda[2], rdb[2];   // fragment addresses of the two 16-byte chunks, current buffers
@@ -331,35 +330,45 @@ __global__ __launch_bounds__(512) void k_gemm_q8_pp(GemmQ8Args a) {
 #define FF_RDS(q)                                                                                                          \
   do {                                                                                                                     \
     const uint32_t ad = rds + (st & 3) * 1024;                                                                             \
-    asm volatile("ds_read2_b32 %0, %1 offset0:%2 offset1:%3" : "=v"(sv[(q) & 1]) : "v"(ad), "n"((q) * 32), "n"((q) * 32 + 16) : "memory"); \
+    asm volatile("ds_read2_b32 %0, %1 offset0:%2 offset1:%3" : "=v"(sv) : "v"(ad), "n"((q) * 32), "n"((q) * 32 + 16) : "memory"); \
   } while (0)
-  f32x2_t sv[2];
-  sv[0] = sv[1] = f32x2_t{0.f, 0.f};
+  f32x2_t sv = {0.f, 0.f};   // the scales of the phase's rows
+  float sp[2] = {0.f, 0.f};  // ... times the weight's
 #define FF_MEM_END() asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory")
-  // the products of phase q's rows, from zero
+  // The products of phase q's rows, from zero, and their scaled addition two products behind, between
+  // the MFMAs; the last two open the next memory part.  Beside additions that stand as a whole in the
+  // memory part this takes 27 registers less and 11% fewer cycles at M = 14566, N = 8192, K = 2048
+  // (598 k for 670 k), of which the time keeps little, 271 us for 272: the clock gives way under the
+  // load (1.90 GHz for 2.09 with every CU at work).  At 4608 x 2048 x 2048 it is 31.9 us for 33.8.
+#define FF_ADD1(q, i)                                                                               \
+  do {                                                                                              \
+    _Pragma("unroll") for (int e = 0; e < 4; ++e)                                                   \
+      acc[2 * (q) + (i) / TN][(i) % TN][e] = fmaf(part[(i) % 3][e], sp[(i) / TN], acc[2 * (q) + (i) / TN][(i) % TN][e]); \
+    FF_TIE(acc[2 * (q) + (i) / TN][(i) % TN]);   /* here, not later: part's registers are free again */ \
+  } while (0)
 #define FF_MMA(q)                                                                                   \
   do {                                                                                              \
     _Pragma("unroll") for (int i = 0; i < 4; ++i) FF_TIE(fa[i]);                                    \
-    FF_TIE(sv[(q) & 1]);                                                                            \
+    FF_TIE(sv);                                                                                     \
+    sp[0] = sv[0] * sw;                                                                             \
+    sp[1] = sv[1] * sw;                                                                             \
     __builtin_amdgcn_sched_barrier(0);                                                              \
     __builtin_amdgcn_s_setprio(1);                                                                  \
-    _Pragma("unroll") for (int t = 0; t < 2; ++t)                                                   \
-      _Pragma("unroll") for (int u = 0; u < TN; ++u)                                                \
-        part[t][u] = mfma_q8(join(fb[2 * u], fb[2 * u + 1]), join(fa[2 * t], fa[2 * t + 1]), f32x4_t{0.f, 0.f, 0.f, 0.f}); \
+    _Pragma("unroll") for (int i = 0; i < 2 * TN; ++i) {                                            \
+      const int t = i / TN, u = i % TN;                                                             \
+      part[i % 3] = mfma_q8(join(fb[2 * u], fb[2 * u + 1]), join(fa[2 * t], fa[2 * t + 1]), f32x4_t{0.f, 0.f, 0.f, 0.f}); \
+      __builtin_amdgcn_sched_barrier(0);                                                            \
+      if (i >= 2) FF_ADD1(q, i - 2);                                                                \
+      __builtin_amdgcn_sched_barrier(0);                                                            \
+    }                                                                                               \
     __builtin_amdgcn_s_setprio(0);                                                                  \
     __builtin_amdgcn_sched_barrier(0);                                                              \
     asm volatile("s_barrier" ::: "memory");                                                         \
   } while (0)
-  // ... and their way into the accumulators, in the next phase's memory part
 #define FF_ADD(q)                                                                                   \
   do {                                                                                              \
-    _Pragma("unroll") for (int t = 0; t < 2; ++t) {                                                 \
-      const float s = sv[(q) & 1][t] * sw;                                                          \
-      _Pragma("unroll") for (int u = 0; u < TN; ++u)                                                \
-        _Pragma("unroll") for (int e = 0; e < 4; ++e) acc[2 * (q) + t][u][e] = fmaf(part[t][u][e], s, acc[2 * (q) + t][u][e]); \
-    }                                                                                               \
-    _Pragma("unroll") for (int t = 0; t < 2; ++t)   /* here, not later: part's registers are free again */ \
-      _Pragma("unroll") for (int u = 0; u < TN; ++u) FF_TIE(acc[2 * (q) + t][u]);                   \
+    FF_ADD1(q, 2 * TN - 2);                                                                         \
+    FF_ADD1(q, 2 * TN - 1);                                                                         \
   } while (0)
   auto stage = [&](auto LEFTc) __attribute__((always_inline)) {
     constexpr int LEFT = decltype(LEFTc)::value;
@@ -373,9 +382,9 @@ __global__ __launch_bounds__(512) void k_gemm_q8_pp(GemmQ8Args a) {
     }
     FF_RDA(0);
     FF_RDS(0);
+    FF_ADD(3);
     if (k1) FF_DMA(ra, voa[3], 3 * PC + oa, kb + RB);
     if (k2) FF_DMAS(st + 2);
-    FF_ADD(3);
     sw = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vsw), st & 63));
     wait_vm<pp_vm(TN, 0, LEFT)>();
     FF_MEM_END();
@@ -385,36 +394,36 @@ __global__ __launch_bounds__(512) void k_gemm_q8_pp(GemmQ8Args a) {
     // phase 1
     FF_RDA(1 * PC);
     FF_RDS(1);
+    FF_ADD(0);
     if (k2) {
       FF_DMA(ra, voa[0], ca, kb + 2 * RB);
       FF_DMA(rw, vob[0], OFFB + cb, kb + 2 * RB);
       FF_DMA(rw, vob[1], OFFB + PC + cb, kb + 2 * RB);
     }
-    FF_ADD(0);
     wait_vm<pp_vm(TN, 1, LEFT)>();
     FF_MEM_END();
     FF_MMA(1);
     // phase 2
     FF_RDA(2 * PC);
     FF_RDS(2);
+    FF_ADD(1);
     if (k2) {
       FF_DMA(ra, voa[1], PC + ca, kb + 2 * RB);
       if (TN > 2) FF_DMA(rw, vob[TN > 2 ? 2 : 0], OFFB + 2 * PC + cb, kb + 2 * RB);
     }
-    FF_ADD(1);
     wait_vm<pp_vm(TN, 2, LEFT)>();
     FF_MEM_END();
     FF_MMA(2);
     // phase 3
     FF_RDA(3 * PC);
     FF_RDS(3);
+    FF_ADD(2);
     rda[0] += oa - ca; rda[1] += oa - ca;
     rdb[0] += ob - cb; rdb[1] += ob - cb;
     if (k2) {
       FF_DMA(ra, voa[2], 2 * PC + ca, kb + 2 * RB);
       if (TN > 3) FF_DMA(rw, vob[TN > 3 ? 3 : 0], OFFB + 3 * PC + cb, kb + 2 * RB);
     }
-    FF_ADD(2);
     wait_vm<pp_vm(TN, 3, LEFT)>();
     FF_MEM_END();
     FF_MMA(3);
@@ -455,6 +464,7 @@ __global__ __launch_bounds__(512) void k_gemm_q8_pp(GemmQ8Args a) {
   FF_ADD(3);
   if (wave < 4) asm volatile("s_barrier" ::: "memory");
 #undef FF_ADD
+#undef FF_ADD1
 #undef FF_MEM_END
 #undef FF_DMA
 #undef FF_DMAS

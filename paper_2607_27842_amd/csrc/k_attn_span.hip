@@ -84,9 +84,10 @@ __device__ __forceinline__ Ranges ranges_of(const Row (&w)[QT]) {
 // The scores of 8 keys from the products p = q . k, key j at k0 + 16 (j / 4) + j % 4: natural units in fp32,
 // log2 units in bf16 (where the exponential is the hardware's exp2 and tanh is formed from exp2 and
 // rcp, a few 1e-7 of the cap off, far below a bf16 probability's rounding).  A finite score stays
-// finite: the type's lowest value in a table is a score like any other.
+// finite: the type's lowest value in a table is a score like any other.  slope, tab: the head's slope or
+// the keys' entries of its table.
 template <bool F32>
-__device__ __forceinline__ void scores(const AttnSpanArgs& a, const Row& w, float (&p)[8], int k0) {
+__device__ __forceinline__ void scores(const AttnSpanArgs& a, const Row& w, float (&p)[8], int k0, float slope, const float (&tab)[8]) {
   if (a.cap > 0.f) {
     const float c1 = F32 ? a.scale / a.cap : 2.f * kLog2e * a.scale / a.cap, c2 = a.cap;
 #pragma unroll
@@ -97,12 +98,11 @@ __device__ __forceinline__ void scores(const AttnSpanArgs& a, const Row& w, floa
     for (int j = 0; j < 8; ++j) p[j] *= a.scale;
   }
   if (a.bias_kind == BIAS_SLOPE) {
-    const float slope = w.bias[0];
 #pragma unroll
     for (int j = 0; j < 8; ++j) p[j] -= slope * fabsf((float)(k0 + 16 * (j / 4) + j % 4 - w.pos));
   } else if (a.bias_kind == BIAS_TABLE) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) p[j] += w.bias[min(max(k0 + 16 * (j / 4) + j % 4 - w.pos, -a.reach), a.reach)];
+    for (int j = 0; j < 8; ++j) p[j] += tab[j];
   }
   if (!F32) {
 #pragma unroll
@@ -131,7 +131,32 @@ __device__ __forceinline__ uint32_t clean_bf16x2(uint32_t w) {
 }
 __device__ __forceinline__ bool odd_f32(float x) { return !(fabsf(x) <= kFltMax); }
 
-// O^T of the merge and of a split's partial result: lane l holds row l % 16, dims 16 e + 4 (l / 16) + 0..3
+// Chunks of 16 dims that stand together: in fp32 a lane loads 4, 2 or 1 neighbouring dims of a V row (as few
+// and wide loads as NE allows), so that chunks c0 .. c0 + W - 1 hold every W-th of 16 W dims each.
+template <bool F32, int NE>
+__host__ __device__ constexpr int chunks_with(int c) { return !F32 ? 1 : c < (NE & ~3) ? 4 : c < (NE & ~1) ? 2 : 1; }
+template <bool F32, int NE>
+__host__ __device__ constexpr int chunk_first(int c) { return !F32 ? c : c < (NE & ~3) ? c & ~3 : c < (NE & ~1) ? NE & ~3 : c; }
+// the dim of o[c][v] in lane l, g = l / 16
+template <bool F32, int NE>
+__device__ __forceinline__ int dim_of(int c, int v, int g) {
+  const int c0 = chunk_first<F32, NE>(c), W = chunks_with<F32, NE>(c);
+  return 16 * c0 + W * (4 * g + v) + c - c0;
+}
+// ... and the first of the four dims that piece c of in_order(o) holds
+template <bool F32, int NE>
+__device__ __forceinline__ int dims_at(int c, int g) {
+  const int c0 = chunk_first<F32, NE>(c), W = chunks_with<F32, NE>(c);
+  return 16 * c0 + 4 * (W * g + c - c0);
+}
+template <bool F32, int NE>
+__device__ __forceinline__ f32x4_t in_order(const f32x4_t (&o)[NE], int c) {
+  const int c0 = chunk_first<F32, NE>(c), W = chunks_with<F32, NE>(c);
+  f32x4_t y;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] = o[c0 + (4 * (c - c0) + e) % W][(4 * (c - c0) + e) / W];
+  return y;
+}
 template <int DT>
 __device__ __forceinline__ void store_o4(void* out, size_t o, f32x4_t v) {
   if (DT == DT_BF16) *reinterpret_cast<u32x2_t*>(reinterpret_cast<uint16_t*>(out) + o) = u32x2_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
@@ -186,7 +211,7 @@ __device__ __forceinline__ void attend16(const AttnSpanArgs& a, const Row& w, co
   const uint32_t kl = (uint32_t)a.kr * (uint32_t)es, vl = (uint32_t)a.vr * (uint32_t)es;
   constexpr int NT = NQ > 2 ? 2 : NQ;           // the last chunks, where d may end
   constexpr bool kStep = !F32 && CPR == 16;     // chunks j lie 4 j rows further
-  uint32_t ko[2], kt[2][NT], vo[F32 ? 4 : kStep ? 1 : NV], vt0 = 0;
+  uint32_t ko[2], kt[2][NT], vo[F32 || kStep ? 1 : NV];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     ko[i] = (16 * i + l16) * kl + EQ * g * (uint32_t)es;
@@ -197,9 +222,7 @@ __device__ __forceinline__ void attend16(const AttnSpanArgs& a, const Row& w, co
     }
   }
   if constexpr (F32) {
-#pragma unroll
-    for (int v = 0; v < 4; ++v) vo[v] = (4 * g + v) * vl + l16 * 4u;
-    vt0 = 16 * vl;
+    vo[0] = 4 * g * vl;
   } else {
 #pragma unroll
     for (int j = 0; j < (kStep ? 1 : NV); ++j) {
@@ -207,26 +230,47 @@ __device__ __forceinline__ void attend16(const AttnSpanArgs& a, const Row& w, co
       vo[j] = e < d ? (idx / CPR) * vl + e * 2u : kOut;
     }
   }
-  auto load = [&](int k0) __attribute__((always_inline)) {
+  constexpr bool kEarly = !F32 || NE <= 6;   // (fp32, d = 128: both steps' K and V do not fit the registers)
+  auto load_k = [&](int k0) __attribute__((always_inline)) {
     const uint32_t last = min(end - k0, kKeys) - 1;
     __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(kp) + (size_t)k0 * kl, 0, last * kl + d * (int)es, 0x00020000);
-    __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(vp) + (size_t)k0 * vl, 0, last * vl + d * (int)es, 0x00020000);
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int c = 0; c < NQ; ++c)
         kf[i][c] = __builtin_amdgcn_raw_buffer_load_b128(rk, c < NQ - NT ? ko[i] + c * DQ * (int)es : kt[i][c < NQ - NT ? 0 : c - (NQ - NT)], 0, 0);
+  };
+  auto load_v = [&](int k0) __attribute__((always_inline)) {
+    const uint32_t last = min(end - k0, kKeys) - 1;
+    __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(vp) + (size_t)k0 * vl, 0, last * vl + d * (int)es, 0x00020000);
     if constexpr (F32) {
+      uint32_t at = vo[0];
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
+      for (int j = 0; j < 8; ++j) {
+        if (j) at += j == 4 ? 13 * vl : vl;
+        FF_TIE(at);   // formed here, one from the other: kept over the loop they would spill
 #pragma unroll
-        for (int c = 0; c < NE; ++c)   // dims past d: what lies there, or zeros; never stored
-          vv[j][c] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rv, vo[j % 4] + (j / 4) * vt0 + c * 64, 0, 0));
+        for (int c = 0; c < NE; c += chunks_with<F32, NE>(c)) {   // dims past d (d % 8 == 0): what lies there, or zeros; never stored
+          const int W = chunks_with<F32, NE>(c);
+          if (W == 4) {
+            const u32x4_t y = __builtin_amdgcn_raw_buffer_load_b128(rv, at + c * 64 + l16 * 16, 0, 0);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) vv[j][c + e < NE ? c + e : 0] = __uint_as_float(y[e]);
+          } else if (W == 2) {
+            const u32x2_t y = __builtin_amdgcn_raw_buffer_load_b64(rv, at + c * 64 + l16 * 8, 0, 0);
+            vv[j][c] = __uint_as_float(y[0]);
+            vv[j][c + 1 < NE ? c + 1 : 0] = __uint_as_float(y[1]);
+          } else {
+            vv[j][c] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rv, at + c * 64 + l16 * 4, 0, 0));
+          }
+        }
+      }
     } else {
 #pragma unroll
       for (int j = 0; j < NV; ++j) vf[j] = __builtin_amdgcn_raw_buffer_load_b128(rv, kStep ? vo[0] + j * 4 * vl : vo[kStep ? 0 : j], 0, 0);
     }
   };
+  const float slope = a.bias_kind == BIAS_SLOPE ? w.bias[0] : 0.f;
 #pragma unroll
   for (int e = 0; e < NE; ++e) o[e] = z4;
   m = -INFINITY;
@@ -238,11 +282,19 @@ __device__ __forceinline__ void attend16(const AttnSpanArgs& a, const Row& w, co
     return k;
   };
   int k0 = next(first);
-  if (k0 < end) load(k0);
+  if (k0 < end) {
+    load_k(k0);
+    load_v(k0);
+  }
   while (k0 < end) {
+    float tab[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (a.bias_kind == BIAS_TABLE) {   // before the next step's loads, which would have to land first
+#pragma unroll
+      for (int j = 0; j < 8; ++j) tab[j] = w.bias[min(max(k0 + 4 * g + 16 * (j / 4) + j % 4 - w.pos, -a.reach), a.reach)];
+    }
     const bool part = !rg.all(k0, kKeys);
     bool odd = false;
-    if (part) {
+    auto look = [&]() __attribute__((always_inline)) {
       Top top;
       if constexpr (F32) {
 #pragma unroll
@@ -269,8 +321,9 @@ __device__ __forceinline__ void attend16(const AttnSpanArgs& a, const Row& w, co
             for (int e = 0; e < 4; ++e) vf[j][e] = clean_bf16x2(vf[j][e]);
         }
       }
-    }
+    };
     if constexpr (!F32) {
+      if (part) look();
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
         const int idx = j * 64 + lane;
@@ -292,12 +345,14 @@ __device__ __forceinline__ void attend16(const AttnSpanArgs& a, const Row& w, co
       }
     const int kk = k0;
     k0 = next(k0 + stride);
-    if constexpr (!F32)
-      if (k0 < end) load(k0);   // K is in the scores, V in LDS
+    if (k0 < end) {   // K is in the scores; V in LDS, or (fp32) still needed
+      if constexpr (kEarly) load_k(k0);
+      if constexpr (!F32) load_v(k0);
+    }
     float p[8], x = -INFINITY;
 #pragma unroll
     for (int j = 0; j < 8; ++j) p[j] = sc[j / 4][j % 4];
-    scores<F32>(a, w, p, kk + 4 * g);
+    scores<F32>(a, w, p, kk + 4 * g, slope, tab);
     if (part) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) p[j] = w.sees(kk + 16 * (j / 4) + 4 * g + j % 4) ? p[j] : -INFINITY;
@@ -318,22 +373,30 @@ __device__ __forceinline__ void attend16(const AttnSpanArgs& a, const Row& w, co
 #pragma unroll
     for (int e = 0; e < NE; ++e) o[e] *= al;
     if constexpr (F32) {
+      if (part) look();
 #pragma unroll
       for (int j = 0; j < 8; ++j)
 #pragma unroll
         for (int c = 0; c < NE; ++c) o[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(vv[j][c], p[j], o[c], 0, 0, 0);
       if (__builtin_expect(odd, 0)) {
-        for (int k = kk; k < min(kk + kKeys, end); ++k)
+        for (int k = kk; k < min(kk + kKeys, end); ++k) {
+          const float* row = reinterpret_cast<const float*>(vp) + (size_t)k * a.vr;
+          const bool sees = w.sees(k);
+          int gd = g;
+          FF_TIE(gd);   // nothing of this is formed ahead of the loop over the steps
 #pragma unroll
-          for (int c = 0; c < NE; ++c) {
-            if (16 * c + 4 * g >= d) continue;
-            const f32x4_t y = *reinterpret_cast<const f32x4_t*>(vp + ((size_t)k * a.vr + 16 * c + 4 * g) * 4);
+          for (int c = 0; c < NE; ++c)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (odd_f32(y[e]) && w.sees(k)) o[c][e] += y[e];
-          }
+            for (int e = 0; e < 4; ++e) {
+              const float y = row[min(dim_of<F32, NE>(c, e, gd), d - 1)];   // (dims past d are never stored)
+              if (odd_f32(y) && sees) o[c][e] += y;
+            }
+        }
       }
-      if (k0 < end) load(k0);
+      if (k0 < end) {
+        if constexpr (!kEarly) load_k(k0);
+        load_v(k0);
+      }
     } else {
       const u32x4_t pw = {pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])};
       // in two halves, for the registers
@@ -447,7 +510,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dir(AttnSpanArgs a, int nsplit)
   if (nsplit > 1) {
     float* pt = a.part + (size_t)blockIdx.x * part_floats(NE);
 #pragma unroll
-    for (int c = 0; c < NE; ++c) *reinterpret_cast<f32x4_t*>(pt + l16 * 16 * NE + 16 * c + 4 * g) = o[c];
+    for (int c = 0; c < NE; ++c) *reinterpret_cast<f32x4_t*>(pt + l16 * 16 * NE + dims_at<F32, NE>(c, g)) = in_order<F32, NE>(o, c);
     if (g == 0) {
       pt[256 * NE + 2 * l16] = m;
       pt[256 * NE + 2 * l16 + 1] = s;
@@ -459,7 +522,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dir(AttnSpanArgs a, int nsplit)
   const size_t oo = (size_t)P.b * a.ob + (size_t)qi * a.orow + (size_t)(P.hk * a.G + qh) * a.oh;
 #pragma unroll
   for (int c = 0; c < NE; ++c)
-    if (16 * c + 4 * g < d) store_o4<DT>(a.out, oo + 16 * c + 4 * g, o[c] * inv);
+    if (dims_at<F32, NE>(c, g) < d) store_o4<DT>(a.out, oo + dims_at<F32, NE>(c, g), in_order<F32, NE>(o, c) * inv);
 #endif
 }
 

@@ -112,8 +112,9 @@ __device__ __forceinline__ void scores(const AttnSpanArgs& a, const Row& w, floa
     }
   }
 }
+// e^t in fp32 (t <= 0: the rounding of t log2(e) is off by no more of t than the score's own, 2^-24), 2^t in bf16
 template <bool F32>
-__device__ __forceinline__ float exp_of(float t) { return F32 ? expf(t) : __builtin_amdgcn_exp2f(t); }
+__device__ __forceinline__ float exp_of(float t) { return __builtin_amdgcn_exp2f(F32 ? t * kLog2e : t); }
 
 // Largest exponents of bf16 pairs / magnitude of fp32 values so far: all ones tell an infinity or a NaN
 typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));

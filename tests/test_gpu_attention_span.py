@@ -171,6 +171,25 @@ def test_unseen_rows_may_hold_anything(dtype, heads, n, d, kind):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("d", [8, 24, 48, 80, 96, 104, 128])
+def test_unseen_rows_by_head_dim(dtype, d):
+    """An infinity in each dim of V, the dims' signs mixed, in keys that part of a step's rows see."""
+    q, k, v = inputs(2, 4, 2, d, 75, 75, dtype)
+    for e in range(d):
+        v[:, 40 + e % 30, e % 2, e] = math.inf if e % 3 else -math.inf
+    v[0, 71, 1, d // 2] = math.nan
+    check(q, k, v, spans_of("causal", 2, 75, 75))
+
+
+@pytest.mark.parametrize("B,H", [(5, 8), (2, 12), (3, 11), (2, 10), (1, 7), (12, 8)])
+@pytest.mark.parametrize("kind", ["causal", None])
+def test_heads_over_the_grid(B, H, kind):
+    """Every head's every row has its place, however the heads divide."""
+    n = 400
+    check(*inputs(B, H, H, 64, n, n, BF), spans_of(kind, B, n, n) if kind else None)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
 @pytest.mark.parametrize("heads,n", [((2, 4, 4), 45), ((2, 4, 4), 700)], ids=str)
 def test_layouts(dtype, heads, n):
     """One projection's [B, N, 3, H, d] result; head-major keys; one sample's keys for all; head-major output

@@ -457,8 +457,8 @@ __device__ __forceinline__ void attend16(const AttnSpanArgs& a, const Row& w, co
 // are split over workgroups too, in equal parts of the rows' own keys.
 // What bounds it: memory on long caches (B = 8 ragged up to 32768 keys, 16 heads on 4 of 128: 67 us and
 // 5 for the join, 4.5 TB/s), latency on short ones (33 tokens 6 us); in fp32 the fp32 MFMA rate and the
-// softmax's vector instructions, which do not run beside them (1500 tokens, 12 heads of 64: 92 us, 75 TFLOP/s; 32 rows a wavefront, with half the loads
-// but two wavefronts a SIMD instead of three, 110).
+// softmax's vector instructions, which do not run beside them (1500 tokens, 12 heads of 64: 92 us, 75
+// TFLOP/s; 32 rows a wavefront, with half the loads but two wavefronts a SIMD instead of three, 110).
 template <int DT, int NE>
 __global__ __launch_bounds__(256, 2) void k_attn_dir(AttnSpanArgs a, int nsplit) {
 #ifdef __HIP_DEVICE_COMPILE__   // the host pass needs the launch stub only
@@ -591,9 +591,9 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnSpanArgs a, int nsplit, i
 // probabilities at once).
 // MOD: capped or biased scores, formed in log2 units before the softmax.
 // What bounds it: as k_attn_pp, whose results it repeats bit for bit without spans, in its time (N =
-// 14566, H = 16, d = 128 1424 us).  With 256 of those rows padded text: 1399 us, 1.20 PFLOP/s.  Short spans
-// are bound by what a workgroup does once, 8 us, and by its partly seen tiles (packed prompts of 4096 tokens
-// with about 600 each, 16 heads on 8: 44 us, 180 TFLOP/s).
+// 14566, H = 16, d = 128 1424 us).  With 256 of those rows padded text: 1400 to 1440 us, 1.18 PFLOP/s.  Short spans
+// are bound by what a workgroup does once, 8 us, and by the softmax of its partly seen tiles (packed prompts of
+// 4096 tokens with about 600 each, 16 heads on 8: 44 us, 180 TFLOP/s; capped 45 to 48).
 // (two workgroups share a CU where a K or V row takes 128 bytes of LDS: at most 128 VGPRs)
 template <int RWB, int NC, int NE, int QT, bool MOD>
 __global__ __launch_bounds__(512, RWB == 128 ? 4 : 2) void k_attn_span_pp(AttnSpanArgs a) {

@@ -433,8 +433,9 @@ ff_status ff_rel_l1(const ff_model_desc* m, const void* a, const void* b, float 
  *
  * The rules of this section and the next, beside those above: rows, M, n_q of 0 queue
  * nothing and succeed (checked like any other call); a buffer's rows lie at its own pitch,
- * and what lies between, behind the last row or in other columns is neither read nor
- * written; outputs overlap no input or other output unless a call says so; the stream and
+ * and what lies between, behind the last row or in other columns is not written and has no
+ * effect; outputs overlap no input or other output unless a call says so (other columns of
+ * one wider buffer, at the same pitch, are no overlap); the stream and
  * all buffers belong to the current device; nothing is kept between calls, so calls on
  * several streams may share inputs, and need workspaces of their own.  Calls may be captured
  * into a graph; one captured call, or ones that follow each other, may share a workspace. */

@@ -17,16 +17,22 @@ constexpr int kMaxRows = 1 << 23;
 
 bool dtype_ok(int dt) { return dt == FF_F32 || dt == FF_BF16; }
 
-// A strided buffer's bytes, first to last
+// A strided buffer's bytes, first to last, and where its rows take `width` bytes every `pitch` (0: no such rows)
 struct Extent {
   const char* p;
-  wide n;
+  wide n, pitch, width;
   bool meets(const Extent& o) const {
-    return p && o.p && n > 0 && o.n > 0 && (wide)(uintptr_t)p < (wide)(uintptr_t)o.p + o.n && (wide)(uintptr_t)o.p < (wide)(uintptr_t)p + n;
+    if (!p || !o.p || n <= 0 || o.n <= 0) return false;
+    const wide at = (wide)(uintptr_t)p, ot = (wide)(uintptr_t)o.p;
+    if (at >= ot + o.n || ot >= at + n) return false;
+    if (pitch <= 0 || pitch != o.pitch) return true;
+    // columns of one wider buffer
+    const wide off = ((ot - at) % pitch + pitch) % pitch;
+    return off < width || off + o.width > pitch;
   }
 };
 Extent rows_of(const void* p, int64_t rows, int64_t cols, int64_t pitch, int es) {
-  return {(const char*)p, rows > 0 && cols > 0 ? ((wide)(rows - 1) * pitch + cols) * es : 0};
+  return {(const char*)p, rows > 0 && cols > 0 ? ((wide)(rows - 1) * pitch + cols) * es : 0, (wide)pitch * es, (wide)cols * es};
 }
 // a pitch of `cols` columns that keeps every row on a multiple of `unit` elements
 bool pitch_ok(int64_t pitch, int64_t cols, int unit) { return pitch >= cols && pitch <= kMaxPitch && pitch % unit == 0; }
@@ -130,7 +136,10 @@ ff_status check_attn(const ff_attn_desc* d) {
 }
 
 Extent attn_extent(const void* p, int64_t B, int64_t sb, int64_t n, int64_t sr, int64_t H, int64_t sh, int64_t d, int es) {
-  return {(const char*)p, B > 0 && n > 0 && H > 0 ? ((wide)(B - 1) * sb + (wide)(n - 1) * sr + (wide)(H - 1) * sh + d) * es : 0};
+  const wide width = (wide)(H - 1) * sh + d;
+  const bool rows = sr >= width && (B == 1 || sb % sr == 0);   // a row's heads stand together, samples whole rows apart
+  return {(const char*)p, B > 0 && n > 0 && H > 0 ? ((wide)(B - 1) * sb + (wide)(n - 1) * sr + width) * es : 0,
+          rows ? (wide)sr * es : 0, width * es};
 }
 
 }  // namespace
@@ -206,7 +215,7 @@ ff_status ff_gemm_q8(const ff_gemm_q8_desc* d, const void* a, const float* a_s, 
                         rows_of(w, d->N, d->K, d->w_row, 1),
                         rows_of(w_s, (d->N + kQBlock - 1) / kQBlock, nb, d->ws_ld, 4),
                         rows_of(bias, 1, d->N, d->N, es), rows_of(resid, d->M, d->N, d->resid_row, es)};
-  const Extent eo = rows_of(out, d->M, d->N, d->out_row, es), ew{(const char*)ws, (wide)need};
+  const Extent eo = rows_of(out, d->M, d->N, d->out_row, es), ew{(const char*)ws, (wide)need, 0, 0};
   for (int i = 0; i < 6; ++i) {
     CHECK(!ew.meets(in[i]), FF_E_SHAPE, "the workspace overlaps an input");
     if (i == 5 && out == resid && d->out_row == d->resid_row) continue;   // each element is read by the lane that writes it
@@ -241,9 +250,9 @@ ff_status ff_attention(const ff_attn_desc* d, const void* q, const void* k, cons
   const Extent in[6] = {attn_extent(q, d->B, d->q_batch, d->n_q, d->q_row, d->H, d->q_head, d->d, es),
                         attn_extent(k, d->B, d->k_batch, d->n_k, d->k_row, d->H_kv, d->k_head, d->d, es),
                         attn_extent(v, d->B, d->v_batch, d->n_k, d->v_row, d->H_kv, d->v_head, d->d, es),
-                        {(const char*)bias, (wide)table * 4}, {(const char*)pos, (wide)d->B * 4},
+                        {(const char*)bias, (wide)table * 4, 0, 0}, {(const char*)pos, (wide)d->B * 4, 0, 0},
                         rows_of(spans, d->n_spans ? d->B : 0, (int64_t)d->n_q * d->n_spans * 2, d->span_batch, 4)};
-  const Extent eo = attn_extent(out, d->B, d->o_batch, d->n_q, d->o_row, d->H, d->o_head, d->d, es), ew{(const char*)ws, (wide)need};
+  const Extent eo = attn_extent(out, d->B, d->o_batch, d->n_q, d->o_row, d->H, d->o_head, d->d, es), ew{(const char*)ws, (wide)need, 0, 0};
   for (const Extent& x : in) {
     CHECK(!eo.meets(x), FF_E_SHAPE, "out overlaps an input");
     CHECK(!ew.meets(x), FF_E_SHAPE, "the workspace overlaps an input");

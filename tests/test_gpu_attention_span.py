@@ -216,6 +216,23 @@ def test_layouts(dtype, heads, n):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("n,d", [(45, 72), (150, 48), (700, 64)])
+def test_output_beside_its_operands(dtype, n, d):
+    """A [B, N, 4, H, d] buffer whose last quarter takes the output; the fp32 kernel's loads of V run into it."""
+    need_gpu()
+    n = 150 if dtype == F32 and n > 200 else n
+    x = O.randn((2, n, 4, 4, d), O.gen(n + d), dtype)
+    x[:, :, 3] = math.nan
+    dx = x.cuda()
+    sp = spans_of("causal", 2, n, n)
+    q, k, v, out = dx.unbind(2)
+    O.attention_call(q, k, v, 0.125, spans=sp.cuda(), out=out)
+    ref, tol = O.attention_ref(*x.unbind(2)[:3], 0.125, spans=sp)
+    O.close(out, ref, tol, "attention")
+    assert torch.equal(dx[:, :, :3].cpu(), x[:, :, :3])
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
 def test_shared_spans_and_no_keys(dtype):
     need_gpu()
     q, k, v = inputs(3, 4, 2, 64, 20, 20, dtype)

@@ -210,6 +210,21 @@ def test_gemm_epilogues(dtype, bias, gelu, resid, M, N, K):
     O.close(got, ref, tol, "gemm")
 
 
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("M,N,K", [(5, 200, 272), (130, 1096, 528), (4500, 2568, 400)])
+def test_gemm_into_other_columns(dtype, M, N, K):
+    """The output beside its residual in one buffer, whose other columns stay."""
+    need_gpu()
+    g = O.gen(M + 1)
+    h, d = operands(M, N, K, g)
+    r = O.randn((M, 2 * N + 8), g, dtype)
+    buf = r.cuda()
+    O.gemm_call(*d, None, False, buf[:, :N], dtype, buf[:, N:2 * N])
+    ref, tol = O.gemm_ref(*h, None, False, r[:, :N], dtype)
+    O.close(buf[:, N:2 * N], ref, tol, "gemm")
+    assert torch.equal(buf[:, :N].cpu(), r[:, :N]) and torch.equal(buf[:, 2 * N:].cpu(), r[:, 2 * N:])
+
+
 def test_gemm_kernels_that_shapes_reach():
     """The sizes above reach every kernel: splits of K where there are few tiles and a long K."""
     need_gpu()

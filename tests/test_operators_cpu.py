@@ -113,6 +113,15 @@ def test_gemm_residual_in_place_needs_the_same_pitch():
     refused(E.FF_E_SHAPE, gemm, dict(out=at(6)), out_row=72)
 
 
+@pytest.mark.parametrize("off", [8, 56, 72, 120, -8, -120])
+def test_columns_of_one_buffer_that_overlap(off):
+    """Rows of 64 columns every 128, `off` columns apart."""
+    refused(E.FF_E_SHAPE, gemm, dict(out=at(6) + 2 * off), out_row=128, resid_row=128)
+    if off > 0:
+        refused(E.FF_E_SHAPE, attn, dict(out=at(1) + 8 * off), q_row=512, o_row=512, q_batch=4096, o_batch=4096)
+        refused(E.FF_E_SHAPE, attn, dict(out=at(2) + 4 * off), k_row=256, o_row=256, k_batch=2048 + 128, o_batch=2048)
+
+
 def test_gemm_workspace():
     big = dict(M=128, N=2048, K=8192, a_row=8192, w_row=8192, out_row=2048, resid_row=2048, as_ld=128, ws_ld=64)
     n = abi.ff_gemm_q8_workspace_bytes(gemm_desc(**big))

@@ -529,11 +529,13 @@ __global__ __launch_bounds__(256, 2) void k_attn_dir(AttnSpanArgs a, int nsplit)
     return;
   }
   if (P.tile * 16 + l16 >= R) return;
-  const float inv = s == 0.f ? 0.f : 1.f / s;   // no key seen: zeros
+  // No key seen, or none with a weight: zeros, also where 0 * V has met an infinity or a NaN
+  const bool none = s == 0.f;
+  const float inv = 1.f / s;
   const size_t oo = (size_t)P.b * a.ob + (size_t)qi * a.orow + (size_t)(P.hk * a.G + qh) * a.oh;
 #pragma unroll
   for (int c = 0; c < NE; ++c)
-    if (dims_at<F32, NE>(c, g) < d) store_o4<DT>(a.out, oo + dims_at<F32, NE>(c, g), in_order<F32, NE>(o, c) * inv);
+    if (dims_at<F32, NE>(c, g) < d) store_o4<DT>(a.out, oo + dims_at<F32, NE>(c, g), none ? f32x4_t{0.f, 0.f, 0.f, 0.f} : in_order<F32, NE>(o, c) * inv);
 #endif
 }
 
@@ -564,7 +566,7 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnSpanArgs a, int nsplit, i
     }
     const float m = wave_max(ms), w = exp_of<DT == DT_F32>(ms - (m == -INFINITY ? 0.f : m)), l = wave_sum(ls * w);
     f[lane] = w;
-    if (lane == 0) linv = l == 0.f ? 0.f : 1.f / l;
+    if (lane == 0) linv = l == 0.f ? 0.f : 1.f / l;   // 0: no split has a weight, zeros below whatever the sums are
   }
   __syncthreads();
   f32x4_t o = {0.f, 0.f, 0.f, 0.f};
@@ -577,7 +579,8 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnSpanArgs a, int nsplit, i
 #pragma unroll
   for (int i = 1; i < 8; ++i) o += part[i][q];
   const int qi = query_of(a, r);
-  store_o4<DT>(a.out, (size_t)b * a.ob + (size_t)qi * a.orow + (size_t)(hk * a.G + r - qi * a.G) * a.oh + 4 * q, o * linv);
+  store_o4<DT>(a.out, (size_t)b * a.ob + (size_t)qi * a.orow + (size_t)(hk * a.G + r - qi * a.G) * a.oh + 4 * q,
+               linv == 0.f ? f32x4_t{0.f, 0.f, 0.f, 0.f} : o * linv);
 }
 
 // ---------------------------------------------------------------- bf16, many rows: two wave groups in turn

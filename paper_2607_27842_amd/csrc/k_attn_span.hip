@@ -16,6 +16,10 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kFltMax = 3.402823466e38f;
 constexpr int kKeys = 32;        // keys per wavefront and step of the direct kernels
 constexpr int kMaxSplit = 64;
+// Largest cap for which bf16 forms cap tanh(t / cap) as cap - 2 cap / (1 + 2^(2 t log2(e) / cap)): near
+// zero that is off by up to 1.3e-7 of the cap, 3e-5 at 256 (0.09 at 1e6, where a probability's rounding is
+// 2^-8).  Above it, tanhf, as in fp32.
+constexpr float kFastCap = 256.f;
 
 // r / G and r % G of a row r < 2^30: mul = ceil(2^(31 + shift) / G) with 2^shift >= G is exact
 __device__ __forceinline__ int query_of(const AttnSpanArgs& a, int r) { return (int)(((uint64_t)(uint32_t)r * a.gmul) >> (31 + a.gshift)); }
@@ -82,17 +86,20 @@ __device__ __forceinline__ Ranges ranges_of(const Row (&w)[QT]) {
 }
 
 // The scores of 8 keys from the products p = q . k, key j at k0 + 16 (j / 4) + j % 4: natural units in fp32,
-// log2 units in bf16 (where the exponential is the hardware's exp2 and tanh is formed from exp2 and
-// rcp, a few 1e-7 of the cap off, far below a bf16 probability's rounding).  A finite score stays
+// log2 units in bf16 (where the exponential is the hardware's exp2, and up to kFastCap tanh is formed from
+// exp2 and rcp, far below a bf16 probability's rounding).  ANY: caps above kFastCap too.  A finite score stays
 // finite: the type's lowest value in a table is a score like any other.  slope, tab: the head's slope or
 // the keys' entries of its table.
-template <bool F32>
+template <bool F32, bool ANY>
 __device__ __forceinline__ void scores(const AttnSpanArgs& a, const Row& w, float (&p)[8], int k0, float slope, const float (&tab)[8]) {
-  if (a.cap > 0.f) {
-    const float c1 = F32 ? a.scale / a.cap : 2.f * kLog2e * a.scale / a.cap, c2 = a.cap;
+  if (ANY && a.cap > (F32 ? 0.f : kFastCap)) {
+    const float c1 = a.scale / a.cap, c2 = a.cap;
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      p[j] = F32 ? c2 * tanhf(c1 * p[j]) : fmaf(-2.f * c2, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(c1 * p[j])), c2);
+    for (int j = 0; j < 8; ++j) p[j] = c2 * tanhf(c1 * p[j]);
+  } else if (a.cap > 0.f) {
+    const float c1 = 2.f * kLog2e * a.scale / a.cap, c2 = a.cap;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) p[j] = fmaf(-2.f * c2, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(c1 * p[j])), c2);
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j) p[j] *= a.scale;
@@ -195,8 +202,8 @@ __device__ __forceinline__ Place place_of(const AttnSpanArgs& a, int nsplit, int
 // one's scores and products are formed.  Rows of V that some queries see and others do not may hold
 // an infinity or a NaN, which must not meet a probability of zero: the product is formed without
 // it, and it is added afterwards to the rows that see its key.
-// Result: m (the same in a row's four lanes), l (to be added over them), o.
-template <int DT, int NE>
+// Result: m (the same in a row's four lanes), l (to be added over them), o.  ANY: of any cap (scores).
+template <int DT, int NE, bool ANY>
 __device__ __forceinline__ void attend16(const AttnSpanArgs& a, const Row& w, const Ranges& rg, const char* qp, const char* kp,
                                          const char* vp, int first, int end, int stride, char* stg, f32x4_t (&o)[NE], float& m, float& l) {
   constexpr bool F32 = DT == DT_F32;
@@ -362,7 +369,7 @@ __device__ __forceinline__ void attend16(const AttnSpanArgs& a, const Row& w, co
     float p[8], x = -INFINITY;
 #pragma unroll
     for (int j = 0; j < 8; ++j) p[j] = sc[j / 4][j % 4];
-    scores<F32>(a, w, p, kk + 4 * g, slope, tab);
+    scores<F32, ANY>(a, w, p, kk + 4 * g, slope, tab);
     if (part) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) p[j] = w.sees(kk + 16 * (j / 4) + 4 * g + j % 4) ? p[j] : -INFINITY;
@@ -490,7 +497,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dir(AttnSpanArgs a, int nsplit)
   const char* vp = (const char*)a.v + ((size_t)P.b * a.vb + (size_t)P.hk * a.vh) * es;
   f32x4_t o[NE];
   float m, l;
-  attend16<DT, NE>(a, w[0], rg, qp, kp, vp, first + wave * kKeys, end, 4 * kKeys, smem + wave * kKeys * PV, o, m, l);
+  attend16<DT, NE, true>(a, w[0], rg, qp, kp, vp, first + wave * kKeys, end, 4 * kKeys, smem + wave * kKeys * PV, o, m, l);
   // the waves' (m, l, O) merge in wave order; l is per lane, m common to a row's four lanes
   float (*xch)[NE * 4 + 2][64] = reinterpret_cast<float (*)[NE * 4 + 2][64]>(smem);
   __syncthreads();   // every wave is done with its staged rows
@@ -592,13 +599,16 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnSpanArgs a, int nsplit, i
 // A workgroup walks the tiles that its rows' spans meet.  Per tile a wave knows whether all its rows
 // see all keys (no mask), some (each score is tested against its row's spans), or none (zero
 // probabilities at once).
-// MOD: capped or biased scores, formed in log2 units before the softmax.
+// MOD: capped or biased scores, formed in log2 units before the softmax; caps above kFastCap have instances
+// of their own (with both in one, tanhf's constants took up to 6 registers of the others' loop, and
+// spilled 2 where there are 128).
 // What bounds it: as k_attn_pp, whose results it repeats bit for bit without spans, in its time (N =
 // 14566, H = 16, d = 128 1424 us).  With 256 of those rows padded text: 1400 to 1440 us, 1.18 PFLOP/s.  Short spans
 // are bound by what a workgroup does once, 8 us, and by the softmax of its partly seen tiles (packed prompts of
 // 4096 tokens with about 600 each, 16 heads on 8: 44 us, 180 TFLOP/s; capped 45 to 48).
 // (two workgroups share a CU where a K or V row takes 128 bytes of LDS: at most 128 VGPRs)
-template <int RWB, int NC, int NE, int QT, bool MOD>
+enum Mod { kModNone, kMod, kModWide };
+template <int RWB, int NC, int NE, int QT, Mod MOD>
 __global__ __launch_bounds__(512, RWB == 128 ? 4 : 2) void k_attn_span_pp(AttnSpanArgs a) {
 #ifdef __HIP_DEVICE_COMPILE__   // the host pass needs the launch stub only
   constexpr int KB = 64, NB = 4;                 // keys per tile, ring depth
@@ -835,7 +845,15 @@ __global__ __launch_bounds__(512, RWB == 128 ? 4 : 2) void k_attn_span_pp(AttnSp
   }
   // sc -> scores in log2 units
   auto modify = [&](int k0) __attribute__((always_inline)) {
-    if (a.cap > 0.f) {
+    if constexpr (MOD == kModWide) {
+      const float c1 = a.scale / a.cap, c2 = a.cap;
+#pragma unroll
+      for (int t = 0; t < QT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) sc[i][t][v] = c2 * tanhf(c1 * sc[i][t][v]);
+    } else if (a.cap > 0.f) {
       const float c1 = 2.f * kLog2e * a.scale / a.cap, c2 = a.cap;
 #pragma unroll
       for (int t = 0; t < QT; ++t)
@@ -1039,7 +1057,7 @@ __global__ __launch_bounds__(512, RWB == 128 ? 4 : 2) void k_attn_span_pp(AttnSp
         const char* qp = (const char*)((const uint16_t*)a.q + (size_t)b * a.qb + (size_t)i * a.qr + (size_t)(hk * a.G + h) * a.qh);
         const int end = max(rt.e0, rt.e1);
         f32x4_t x[NE];
-        attend16<DT_BF16, NE>(a, w[0], rt, qp, kp, vp, end > 0 ? min(rt.h0, rt.h1) & ~(kKeys - 1) : 0, end, kKeys,
+        attend16<DT_BF16, NE, MOD == kModWide>(a, w[0], rt, qp, kp, vp, end > 0 ? min(rt.h0, rt.h1) & ~(kKeys - 1) : 0, end, kKeys,
                               smem + wave * kOwn, x, m[t], l[t]);
 #pragma unroll
         for (int e = 0; e < NE; ++e) o[e][t] = x[e];
@@ -1080,7 +1098,7 @@ int splits(long tiles, int n_k) {
   return (int)(n < 1 ? 1 : n > kMaxSplit ? kMaxSplit : n);
 }
 int pieces(int d) { return d <= 32 ? 2 : d <= 48 ? 3 : d <= 64 ? 4 : d <= 80 ? 5 : d <= 96 ? 6 : 8; }
-template <bool MOD>
+template <Mod MOD>
 hipError_t launch_pp_mod(const AttnSpanArgs& a, hipStream_t s) {
   // 16 rows a wave for d <= 64 (two workgroups then share a CU); above, 16 or 32, as k_attn_pp
   const long hb = (long)a.H_kv * a.B, R = (long)a.n_q * a.G, w2 = (R + 255) / 256 * hb, w1 = (R + 127) / 128 * hb;
@@ -1103,7 +1121,8 @@ hipError_t launch_pp_mod(const AttnSpanArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 hipError_t launch_pp(const AttnSpanArgs& a, hipStream_t s) {
-  return a.cap > 0.f || a.bias_kind != BIAS_NONE ? launch_pp_mod<true>(a, s) : launch_pp_mod<false>(a, s);
+  if (a.cap > kFastCap) return launch_pp_mod<kModWide>(a, s);
+  return a.cap > 0.f || a.bias_kind != BIAS_NONE ? launch_pp_mod<kMod>(a, s) : launch_pp_mod<kModNone>(a, s);
 }
 long tiles16(int B, int H_kv, int G, int n_q) { return (long)B * H_kv * (((long)n_q * G + 15) / 16); }
 

@@ -520,7 +520,7 @@ enum { FF_BIAS_NONE = 0, FF_BIAS_SLOPE = 1, FF_BIAS_TABLE = 2 };
 
 /* B >= 1, H % H_kv == 0, d in [8, 128] and d % 8 == 0, n_q, n_k >= 0, n_q H B and n_k below 2^30,
  * B H_kv ceil(n_q (H / H_kv) / 16) below 2^23; strides non-negative multiples of 8, out's rows apart from each other; 64 key or value rows
- * within 2^31 bytes; scale > 0, cap >= 0, both finite; 0 <= bias_reach <= 2^20; n_spans 0, 1 or 2. */
+ * within 2^31 bytes; scale in [2^-60, 2^60], cap 0 or in [2^-60, 2^60]; 0 <= bias_reach <= 2^20; n_spans 0, 1 or 2. */
 typedef struct {
   int32_t dtype, B, H, H_kv, d, n_q, n_k;
   int32_t bias_kind, bias_reach, n_spans;

@@ -14,6 +14,7 @@ typedef __int128 wide;
 constexpr int64_t kMaxPitch = (int64_t)1 << 40;   // products with row counts stay inside 128 bits
 // Rows of a call: a launch has fewer than 2^32 threads, and up to 256 of them work on a row
 constexpr int kMaxRows = 1 << 23;
+constexpr float kLeastScale = 0x1p-60f;
 
 bool dtype_ok(int dt) { return dt == FF_F32 || dt == FF_BF16; }
 
@@ -126,8 +127,9 @@ ff_status check_attn(const ff_attn_desc* d) {
   CHECK((wide)d->k_row * es * 64 < 0x7fffff00ll && (wide)d->v_row * es * 64 < 0x7fffff00ll, FF_E_SHAPE,
         "64 key or value rows must lie within 2^31 bytes");
   CHECK(apart(d->o_batch, d->B, d->o_row, d->n_q, d->o_head, d->H, d->d), FF_E_SHAPE, "out's rows overlap each other");
-  CHECK(d->scale > 0.f && isfinite(d->scale), FF_E_RANGE, "scale must be > 0");
-  CHECK(d->cap >= 0.f && isfinite(d->cap), FF_E_RANGE, "cap must be finite and >= 0");
+  // scale / cap has to be a normal number: an infinite one would make a score of zero NaN
+  CHECK(d->scale >= kLeastScale && d->scale <= 1.f / kLeastScale, FF_E_RANGE, "scale must be in [2^-60, 2^60]");
+  CHECK(d->cap == 0.f || (d->cap >= kLeastScale && d->cap <= 1.f / kLeastScale), FF_E_RANGE, "cap must be 0 or in [2^-60, 2^60]");
   CHECK(d->bias_kind >= FF_BIAS_NONE && d->bias_kind <= FF_BIAS_TABLE, FF_E_RANGE, "bias_kind=%d unknown", d->bias_kind);
   CHECK(d->bias_kind != FF_BIAS_TABLE || (d->bias_reach >= 0 && d->bias_reach <= 1 << 20), FF_E_RANGE, "bias_reach=%d outside [0, 2^20]", d->bias_reach);
   CHECK(d->n_spans >= 0 && d->n_spans <= 2, FF_E_RANGE, "n_spans=%d must be 0, 1 or 2", d->n_spans);

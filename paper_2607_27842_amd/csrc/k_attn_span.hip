@@ -1099,16 +1099,12 @@ int splits(long tiles, int n_k) {
 }
 int pieces(int d) { return d <= 32 ? 2 : d <= 48 ? 3 : d <= 64 ? 4 : d <= 80 ? 5 : d <= 96 ? 6 : 8; }
 template <Mod MOD>
-hipError_t launch_pp_mod(const AttnSpanArgs& a, hipStream_t s) {
-  // 16 rows a wave for d <= 64 (two workgroups then share a CU); above, 16 or 32, as k_attn_pp
-  const long hb = (long)a.H_kv * a.B, R = (long)a.n_q * a.G, w2 = (R + 255) / 256 * hb, w1 = (R + 127) / 128 * hb;
-  // (32 with capped or biased scores does not fit the registers)
-  const bool two = !MOD && a.d > 64 && (double)((w2 + 255) / 256) <= 0.63 * ((w1 + 255) / 256);
-  const long nwg = two ? w2 : w1;
+hipError_t launch_pp_mod(const AttnSpanArgs& a, bool two, hipStream_t s) {
+  const long nwg = ((long)a.n_q * a.G + (two ? 255 : 127)) / (two ? 256 : 128) * a.H_kv * a.B;
   if (nwg > 0x7fffffffL) return hipErrorInvalidValue;
 #define FF_ATTN(RWB, NC, NE)                                                                                       \
   do {                                                                                                             \
-    if constexpr (RWB > 128 && !MOD)                                                                               \
+    if constexpr (RWB > 128 && MOD == kModNone)                                                                    \
       if (two) { FF_LAUNCH((k_attn_span_pp<RWB, NC, NE, 2, MOD>), (unsigned)nwg, 512, 0, s, a); break; }           \
     FF_LAUNCH((k_attn_span_pp<RWB, NC, NE, 1, MOD>), (unsigned)nwg, 512, 0, s, a);                                 \
   } while (0)
@@ -1120,34 +1116,39 @@ hipError_t launch_pp_mod(const AttnSpanArgs& a, hipStream_t s) {
 #undef FF_ATTN
   return hipGetLastError();
 }
-hipError_t launch_pp(const AttnSpanArgs& a, hipStream_t s) {
-  if (a.cap > kFastCap) return launch_pp_mod<kModWide>(a, s);
-  return a.cap > 0.f || a.bias_kind != BIAS_NONE ? launch_pp_mod<kMod>(a, s) : launch_pp_mod<kModNone>(a, s);
+bool modified(const AttnSpanArgs& a) { return a.cap > 0.f || a.bias_kind != BIAS_NONE; }
+hipError_t launch_pp(const AttnSpanArgs& a, bool two, hipStream_t s) {
+  if (a.cap > kFastCap) return launch_pp_mod<kModWide>(a, two, s);
+  return modified(a) ? launch_pp_mod<kMod>(a, two, s) : launch_pp_mod<kModNone>(a, two, s);
 }
 long tiles16(int B, int H_kv, int G, int n_q) { return (long)B * H_kv * (((long)n_q * G + 15) / 16); }
 
-// The splits of the direct kernel's keys, or 0 for k_attn_span_pp, by estimated time (us; all keys seen),
+}  // namespace
+
+// The splits of the direct kernel's keys, or k_attn_span_pp, by estimated time (us; all keys seen),
 // fitted to 1 to 16 heads of 64 and 128, 16 to 1000 tokens, B 1 to 8.  The direct kernel: 1.9 for each 128
 // keys of a workgroup or 6.5e-3 for each of all workgroups' together; k_attn_span_pp: 1.1 (0.8 for d <= 64)
 // for each 64 keys and round of workgroups.
 //   B = 1, 16 heads of 128: 33 tokens 5.9 against 8.2 us, 256 tokens 9.0 against 10.3, 640 26 against 16
 //   B = 4, 16 heads of 128: 64 tokens 6.1 against 7.6, 128 tokens 10.8 against 8.8, 1000 163 against 44
-int plan(int dtype, int B, int H_kv, int G, int d, int n_q, int n_k) {
+// k_attn_span_pp takes 16 rows a wave for d <= 64 (two workgroups then share a CU); above, 16 or 32, as
+// k_attn_pp (32 with capped or biased scores does not fit the registers).
+SpanPlan attention_span_plan(int dtype, int B, int H_kv, int G, int d, int n_q, int n_k, int mod) {
   const long t = tiles16(B, H_kv, G, n_q);
   const int n = splits(t, n_k);
-  if (dtype == DT_F32) return n;
+  if (dtype == DT_F32) return SpanPlan{16, n};
   const double turns = (double)((n_k + 127) / 128), chain = 1.9 * turns / n, work = 6.5e-3 * t * turns;
   const double dir = 5.0 + (chain > work ? chain : work) + (n > 1 ? 5.0 : 0.0);
-  const long wg = (long)B * H_kv * (((long)n_q * G + 127) / 128), at_once = d <= 64 ? 512 : 256;
-  const double pp = 6.3 + (d <= 64 ? 0.8 : 1.1) * ((n_k + 63) / 64) * ((wg + at_once - 1) / at_once);
-  return dir <= pp ? n : 0;
+  const long hb = (long)B * H_kv, R = (long)n_q * G, w1 = (R + 127) / 128 * hb, w2 = (R + 255) / 256 * hb;
+  const long at_once = d <= 64 ? 512 : 256;
+  const double pp = 6.3 + (d <= 64 ? 0.8 : 1.1) * ((n_k + 63) / 64) * ((w1 + at_once - 1) / at_once);
+  if (dir <= pp) return SpanPlan{16, n};
+  return SpanPlan{!mod && d > 64 && (double)((w2 + 255) / 256) <= 0.63 * ((w1 + 255) / 256) ? 32 : 16, 0};
 }
-
-}  // namespace
 
 size_t attention_span_workspace(int dtype, int B, int H_kv, int G, int d, int n_q, int n_k) {
   if (n_q <= 0) return 0;
-  const int n = plan(dtype, B, H_kv, G, d, n_q, n_k);
+  const int n = attention_span_plan(dtype, B, H_kv, G, d, n_q, n_k, 0).splits;   // (the same for any scores)
   return n > 1 ? (size_t)tiles16(B, H_kv, G, n_q) * n * part_floats(pieces(d)) * 4 : 0;
 }
 
@@ -1157,8 +1158,9 @@ hipError_t attention_span(int dtype, const AttnSpanArgs& args, hipStream_t s) {
   while ((1L << a.gshift) < a.G) ++a.gshift;
   a.gmul = (uint32_t)(((1ull << (31 + a.gshift)) + a.G - 1) / a.G);
   const long t = tiles16(a.B, a.H_kv, a.G, a.n_q);
-  const int n = plan(dtype, a.B, a.H_kv, a.G, a.d, a.n_q, a.n_k), ne = pieces(a.d);
-  if (n == 0) return launch_pp(a, s);
+  const SpanPlan p = attention_span_plan(dtype, a.B, a.H_kv, a.G, a.d, a.n_q, a.n_k, modified(a));
+  const int n = p.splits, ne = pieces(a.d);
+  if (n == 0) return launch_pp(a, p.rows == 32, s);
   if (t * n > 0x7fffffffL) return hipErrorInvalidValue;
 #define FF_DIR(DT, NE) FF_LAUNCH((k_attn_dir<DT, NE>), (unsigned)(t * n), 256, 0, s, a, n)
 #define FF_DIR_D(DT)                   \

@@ -749,10 +749,9 @@ __global__ __launch_bounds__(256) void k_gemm_q8_join(GemmQ8Args a, int splits) 
 }
 
 // ---------------------------------------------------------------- choice
-enum Kind { kDir, kTwo64, kTwo128, kPP };
-struct Plan { Kind kind; int splits; };
-
 long tiles(long M, long N, long t) { return ((M + t - 1) / t) * ((N + t - 1) / t); }
+
+}  // namespace
 
 // The kernel of a shape by estimated time (us), fitted to 25 shapes of 1 to 4608 rows, N and K of 1152 to
 // 8192.  A tile of 64 x 64 takes 0.21 us per block of K while each CU has one, 0.5 with two on every CU;
@@ -762,46 +761,48 @@ long tiles(long M, long N, long t) { return ((M + t - 1) / t) * ((N + t - 1) / t
 //   M 128 N 2048 K 8192: 64 x 64 tiles 17.7 us, with 2 / 4 / 8 splits 14.2 / 12.4 / 14.7
 //   M 512 N 8192 K 2048: 128 x 128 14.9 us, 64 x 64 20.9, 256 x 256 31.9
 //   M 14566 N 8192 K 2048: 256 x 256 263 us, 128 x 128 322, 64 x 64 444
-Plan plan(int dt, int M, int N, int K) {
+Q8Plan gemm_q8_plan(int dt, int M, int N, int K) {
   const int nk = (K + kQBlock - 1) / kQBlock;
   // us per block of K: few tiles, what 256 tiles add, and a round of all CUs (512 tiles of 64 x 64)
   const double c64[2][3] = {{0.21, 0.08, 0.50}, {0.30, 0.12, 0.71}}, c128[2][3] = {{0.42, 0.30, 0.71}, {0.73, 0.40, 1.13}};
   const double *c6 = c64[dt == DT_F32], *c12 = c128[dt == DT_F32];
-  Plan best{kTwo128, 1};
+  Q8Plan best{Q8_TILE128, 1};
   double least = 1e30;
-  auto take = [&](Kind k, int splits, double us) {
-    if (us < least) { least = us; best = Plan{k, splits}; }
+  auto take = [&](int k, int splits, double us) {
+    if (us < least) { least = us; best = Q8Plan{k, splits}; }
   };
   if (M <= 256) {
     const double t = (double)tiles(M, N, 16), chain = 0.4 * ((nk + 15) / 16);
-    take(kDir, 1, 2.5 + (t * nk * 0.45e-3 > chain ? t * nk * 0.45e-3 : chain));
+    take(Q8_DIR, 1, 2.5 + (t * nk * 0.45e-3 > chain ? t * nk * 0.45e-3 : chain));
   }
   for (int s = 1; s <= 8; s *= 2) {
     if (s > 1 && nk / s < 8) break;
     const double t = (double)tiles(M, N, 64) * s, nb = (double)nk / s;
     const double main = t <= 256 ? (c6[0] + c6[1] * t / 256) * nb : ceil(t / 512) * c6[2] * nb;
-    take(kTwo64, s, 3.5 + main + (s > 1 ? 1.8 + s * (0.35 + 2.3e-6 * M * N) : 0.0));
+    take(Q8_TILE64, s, 3.5 + main + (s > 1 ? 1.8 + s * (0.35 + 2.3e-6 * M * N) : 0.0));
   }
   const double t128 = (double)tiles(M, N, 128), t256 = (double)tiles(M, N, 256);
-  take(kTwo128, 1, 3.5 + (t128 <= 256 ? c12[0] + c12[1] * t128 / 256 : ceil(t128 / 256) * c12[2]) * nk);
-  if (dt == DT_BF16 && nk >= 3) take(kPP, 1, 4.0 + ceil(t256 / 256) * 1.95 * nk);
+  take(Q8_TILE128, 1, 3.5 + (t128 <= 256 ? c12[0] + c12[1] * t128 / 256 : ceil(t128 / 256) * c12[2]) * nk);
+  if (dt == DT_BF16 && nk >= 3) take(Q8_TILE256, 1, 4.0 + ceil(t256 / 256) * 1.95 * nk);
   return best;
 }
 
+namespace {
+
 template <int DT>
 hipError_t launch_q8(const GemmQ8Args& a, hipStream_t s) {
-  const Plan p = plan(DT, a.M, a.N, a.K);
-  switch (p.kind) {
-    case kDir: {
+  const Q8Plan p = gemm_q8_plan(DT, a.M, a.N, a.K);
+  switch (p.kernel) {
+    case Q8_DIR: {
       // 16 waves where 8 would take their blocks in two rounds on a part of the CUs
       const long t = tiles(a.M, a.N, 16);
       if (a.K > 32 * kQBlock && t <= 256) FF_LAUNCH((k_gemm_q8_dir<DT, 16>), (unsigned)t, 1024, 0, s, a);
       else FF_LAUNCH((k_gemm_q8_dir<DT, 8>), (unsigned)t, 512, 0, s, a);
       break;
     }
-    case kTwo64: FF_LAUNCH((k_gemm_q8_two<DT, 64, 64, 2>), (unsigned)(tiles(a.M, a.N, 64) * p.splits), 512, 0, s, a, p.splits); break;
-    case kTwo128: FF_LAUNCH((k_gemm_q8_two<DT, 128, 128, 2>), (unsigned)tiles(a.M, a.N, 128), 512, 0, s, a, 1); break;
-    case kPP:
+    case Q8_TILE64: FF_LAUNCH((k_gemm_q8_two<DT, 64, 64, 2>), (unsigned)(tiles(a.M, a.N, 64) * p.splits), 512, 0, s, a, p.splits); break;
+    case Q8_TILE128: FF_LAUNCH((k_gemm_q8_two<DT, 128, 128, 2>), (unsigned)tiles(a.M, a.N, 128), 512, 0, s, a, 1); break;
+    case Q8_TILE256:
       if constexpr (DT == DT_BF16) FF_LAUNCH(k_gemm_q8_pp<4>, (unsigned)tiles(a.M, a.N, 256), 512, 0, s, a);
       break;
   }
@@ -816,7 +817,7 @@ hipError_t launch_q8(const GemmQ8Args& a, hipStream_t s) {
 
 size_t gemm_q8_workspace(int out_dtype, int M, int N, int K) {
   if (M <= 0) return 0;
-  const int n = plan(out_dtype, M, N, K).splits;
+  const int n = gemm_q8_plan(out_dtype, M, N, K).splits;
   return n > 1 ? (size_t)n * M * N * 4 : 0;
 }
 

@@ -175,6 +175,10 @@ struct GemmQ8Args {
   int M, N, K, gelu;
   float* part;   // workspace: gemm_q8_workspace bytes
 };
+// What a shape is run with: a kernel (its tile), and workgroups that share a tile's K
+enum { Q8_DIR, Q8_TILE64, Q8_TILE128, Q8_TILE256 };
+struct Q8Plan { int kernel, splits; };
+Q8Plan gemm_q8_plan(int out_dtype, int M, int N, int K);
 size_t gemm_q8_workspace(int out_dtype, int M, int N, int K);
 hipError_t gemm_q8(int out_dtype, const GemmQ8Args& a, hipStream_t s);
 
@@ -191,6 +195,10 @@ struct AttnSpanArgs {
   uint32_t gmul; int gshift;   // r / G = r gmul >> 31 + gshift (set by attention_span)
   float* part;   // workspace: attention_span_workspace bytes
 };
+// What a shape is run with: rows a wavefront holds, and workgroups that share a row's keys in the direct
+// kernel (0: the tiled kernel).  mod: capped or biased scores
+struct SpanPlan { int rows, splits; };
+SpanPlan attention_span_plan(int dtype, int B, int H_kv, int G, int d, int n_q, int n_k, int mod);
 size_t attention_span_workspace(int dtype, int B, int H_kv, int G, int d, int n_q, int n_k);
 hipError_t attention_span(int dtype, const AttnSpanArgs& a, hipStream_t s);
 

@@ -226,11 +226,11 @@ __device__ __forceinline__ void tile_at(int wg, int n, int tiles_m, int tiles_n,
 }
 
 // ---------------------------------------------------------------- large grids: two wave groups in turn
-// 256 x 64 TN tile, a stage of one 128-wide block of K, 8 waves in two groups of four, one wave of
-// each group per SIMD; a stage has four phases, one per 32 rows of a wave's 128 x 16 TN block.  A
-// phase is a memory part (fragment reads, DMA) and 2 TN MFMAs among the fused multiply-adds that scale
+// 256 x 256 tile, a stage of one 128-wide block of K, 8 waves in two groups of four, one wave of
+// each group per SIMD; a stage has four phases, one per 32 rows of a wave's 128 x 64 block.  A
+// phase is a memory part (fragment reads, DMA) and 8 MFMAs among the fused multiply-adds that scale
 // their sums into the accumulators, with a barrier after each; the second group runs half a phase
-// behind, so that on every SIMD one wave's MFMAs (64 TN cycles) cover the other's reads and DMA.
+// behind, so that on every SIMD one wave's MFMAs (256 cycles) cover the other's reads and DMA.
 //
 // Operands: 64-row pieces of 8 KB, each filled by one DMA instruction per wave, in two buffers per
 // operand, and the 256 rows' scales of a stage (1 KB, one 4-byte DMA a lane; waves w and w + 4 write
@@ -246,13 +246,13 @@ __device__ __forceinline__ void tile_at(int wg, int n, int tiles_m, int tiles_n,
 constexpr int kPPIssue[4][3] = {{3, 8, -1}, {0, 4, 5}, {1, 6, -1}, {2, 7, -1}};   // A0-A3, B0-B3, scales
 // How many of a wave's DMAs may be outstanding at the end of phase p of a stage with `left` stages
 // after it (2: two or more), so that what phase p + 1 reads has landed.
-constexpr int pp_vm(int TN, int p, int left) {
+constexpr int pp_vm(int p, int left) {
   int n = 0, need = -1;
   for (int j = -2; j <= 0; ++j)
     for (int q = 0; q < (j == 0 ? p + 1 : 4); ++q)
       for (int i = 0; i < 3; ++i) {
         const int pc = kPPIssue[q][i], st = pc == 3 ? j + 1 : j + 2;
-        if (pc < 0 || (pc < 8 && pc >= 4 + TN) || st > left) continue;
+        if (pc < 0 || st > left) continue;
         ++n;
         const bool next = (p == 0 && pc == 1 && st == 0) || (p == 1 && pc == 2 && st == 0) ||
                           (p == 2 && pc == 3 && st == 0) || (p == 3 && (pc == 0 || pc >= 4) && st == 1);
@@ -261,10 +261,9 @@ constexpr int pp_vm(int TN, int p, int left) {
   return need < 0 ? 63 : n - need;
 }
 
-template <int TN>
 __global__ __launch_bounds__(512) void k_gemm_q8_pp(GemmQ8Args a) {
 #ifdef __HIP_DEVICE_COMPILE__   // the host pass needs the launch stub only
-  constexpr int BM = 256, BN = 64 * TN, WN = 16 * TN, RB = kQBlock;   // RB: bytes of an LDS row
+  constexpr int BM = 256, BN = 256, TN = 4, WN = 16 * TN, RB = kQBlock;   // RB: bytes of an LDS row
   constexpr int PC = 64 * RB, BUFA = 4 * PC, BUFB = TN * PC, OFFB = 2 * BUFA, OFFS = OFFB + 2 * BUFB;
   constexpr int kMain = OFFS + 4 * 1024, kEpi = 8 * 32 * (WN + 4) * 4;
   __shared__ __attribute__((aligned(1024))) char lds[kMain > kEpi ? kMain : kEpi];
@@ -386,7 +385,7 @@ __global__ __launch_bounds__(512) void k_gemm_q8_pp(GemmQ8Args a) {
     if (k1) FF_DMA(ra, voa[3], 3 * PC + oa, kb + RB);
     if (k2) FF_DMAS(st + 2);
     sw = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vsw), st & 63));
-    wait_vm<pp_vm(TN, 0, LEFT)>();
+    wait_vm<pp_vm(0, LEFT)>();
     FF_MEM_END();
 #pragma unroll
     for (int i = 0; i < 2 * TN; ++i) FF_TIE(fb[i]);
@@ -400,7 +399,7 @@ __global__ __launch_bounds__(512) void k_gemm_q8_pp(GemmQ8Args a) {
       FF_DMA(rw, vob[0], OFFB + cb, kb + 2 * RB);
       FF_DMA(rw, vob[1], OFFB + PC + cb, kb + 2 * RB);
     }
-    wait_vm<pp_vm(TN, 1, LEFT)>();
+    wait_vm<pp_vm(1, LEFT)>();
     FF_MEM_END();
     FF_MMA(1);
     // phase 2
@@ -409,9 +408,9 @@ __global__ __launch_bounds__(512) void k_gemm_q8_pp(GemmQ8Args a) {
     FF_ADD(1);
     if (k2) {
       FF_DMA(ra, voa[1], PC + ca, kb + 2 * RB);
-      if (TN > 2) FF_DMA(rw, vob[TN > 2 ? 2 : 0], OFFB + 2 * PC + cb, kb + 2 * RB);
+      FF_DMA(rw, vob[2], OFFB + 2 * PC + cb, kb + 2 * RB);
     }
-    wait_vm<pp_vm(TN, 2, LEFT)>();
+    wait_vm<pp_vm(2, LEFT)>();
     FF_MEM_END();
     FF_MMA(2);
     // phase 3
@@ -422,9 +421,9 @@ __global__ __launch_bounds__(512) void k_gemm_q8_pp(GemmQ8Args a) {
     rdb[0] += ob - cb; rdb[1] += ob - cb;
     if (k2) {
       FF_DMA(ra, voa[2], 2 * PC + ca, kb + 2 * RB);
-      if (TN > 3) FF_DMA(rw, vob[TN > 3 ? 3 : 0], OFFB + 3 * PC + cb, kb + 2 * RB);
+      FF_DMA(rw, vob[3], OFFB + 3 * PC + cb, kb + 2 * RB);
     }
-    wait_vm<pp_vm(TN, 3, LEFT)>();
+    wait_vm<pp_vm(3, LEFT)>();
     FF_MEM_END();
     FF_MMA(3);
     kb += RB;
@@ -438,10 +437,10 @@ __global__ __launch_bounds__(512) void k_gemm_q8_pp(GemmQ8Args a) {
 #pragma unroll
     for (int q = 0; q < 12; ++q) {
       const int pc = kPPIssue[q / 3][q % 3], s = pc == 3 ? j + 1 : j + 2;
-      if (pc < 0 || (pc < 8 && pc >= 4 + TN) || s < 0) continue;
+      if (pc < 0 || s < 0) continue;
       if (pc == 8) FF_DMAS(s);
       else if (pc < 4) FF_DMA(ra, voa[pc & 3], s * BUFA + pc * PC, s * RB);
-      else FF_DMA(rw, vob[pc - 4 < TN ? pc - 4 : 0], OFFB + s * BUFB + (pc - 4) * PC, s * RB);
+      else FF_DMA(rw, vob[pc & 3], OFFB + s * BUFB + (pc - 4) * PC, s * RB);
     }
   wait_vm<4 + TN>();   // stage 0 has landed, and stage 1 but for A3 is on its way
   asm volatile("s_barrier" ::: "memory");
@@ -493,7 +492,7 @@ template <int DT, int BM, int BN, int NS>
 __global__ __launch_bounds__(512) void k_gemm_q8_two(GemmQ8Args a, int splits) {
 #ifdef __HIP_DEVICE_COMPILE__   // the host pass needs the launch stub only
   constexpr int TM = BM / 32, TN = BN / 32, WN = BN / 2, RB = kQBlock;
-  constexpr int STB = (BM + BN) * RB, SCB = BM < 256 ? 256 * ((BM + 63) / 64) : 1024;   // bytes of a block, of its rows' scales
+  constexpr int STB = (BM + BN) * RB, SCB = BM * 4;   // bytes of a block, of its rows' scales
   constexpr int NA = BM / 32, NW = BN / 32, PER = NA + NW + 1;   // DMA instructions of a wave and block
   constexpr int OFFS = 2 * NS * STB, kMain = OFFS + 2 * NS * SCB;
   constexpr int HT = TM / 2, kXch = 8 * HT * TN * 1024, RE = HT > 1 ? 32 : 16, kEpi = kXch + 8 * RE * (WN + 4) * 4;
@@ -525,7 +524,7 @@ __global__ __launch_bounds__(512) void k_gemm_q8_two(GemmQ8Args a, int splits) {
     if ((int)ch >= a.K - (nk - 1) * kQBlock) cut |= 1u << j;
   }
   const uint32_t vos = (uint32_t)min((w * 64 + lane) % BM, a.M - 1 - m0) * 4u, sstep = (uint32_t)a.as_ld * 4u;
-  constexpr int SW = BM / 64 > 0 ? BM / 64 : 1;   // waves whose scales differ; the others repeat them
+  constexpr int SW = BM / 64;   // waves whose scales differ; the others repeat them
   char* const ring = lds + grp * NS * STB;
   char* const sring = lds + OFFS + grp * NS * SCB;
   auto issue1 = [&](int i, int slot, int j) __attribute__((always_inline)) {   // DMA j of the group's block i
@@ -803,7 +802,7 @@ hipError_t launch_q8(const GemmQ8Args& a, hipStream_t s) {
     case Q8_TILE64: FF_LAUNCH((k_gemm_q8_two<DT, 64, 64, 2>), (unsigned)(tiles(a.M, a.N, 64) * p.splits), 512, 0, s, a, p.splits); break;
     case Q8_TILE128: FF_LAUNCH((k_gemm_q8_two<DT, 128, 128, 2>), (unsigned)tiles(a.M, a.N, 128), 512, 0, s, a, 1); break;
     case Q8_TILE256:
-      if constexpr (DT == DT_BF16) FF_LAUNCH(k_gemm_q8_pp<4>, (unsigned)tiles(a.M, a.N, 256), 512, 0, s, a);
+      if constexpr (DT == DT_BF16) FF_LAUNCH(k_gemm_q8_pp, (unsigned)tiles(a.M, a.N, 256), 512, 0, s, a);
       break;
   }
   hipError_t e = hipGetLastError();

@@ -432,7 +432,7 @@ ff_status ff_rel_l1(const ff_model_desc* m, const void* a, const void* b, float 
  * The last block of a direction holds what is left.  All pitches count elements.
  *
  * The rules of this section and the next, beside those above: rows, M, n_q of 0 queue
- * nothing and succeed (checked like any other call); a buffer's rows lie at its own pitch,
+ * nothing and succeed (their descriptors checked like any other); a buffer's rows lie at its own pitch,
  * and what lies between, behind the last row or in other columns is not written and has no
  * effect; outputs overlap no input or other output unless a call says so (other columns of
  * one wider buffer, at the same pitch, are no overlap); the stream and
@@ -483,11 +483,14 @@ typedef struct {
 /* out [M, N] <- act(A W^T + bias) + resid, A [M, K] in 8 bits with scales a_s (blocks of rows),
  * W [N, K] with scales w_s (squares):
  *     (A W^T)[m, n] = sum_b a_s[b, m] w_s[n / 128, b] sum_{k in block b} a[m, k] w[n, k],
- * sums over blocks in fp32, one rounding to out_dtype.  Within a block, fp32 outputs take exact
- * products summed in fp32; bf16 outputs take the 8-bit matrix instructions, which align a block's
- * products to fewer bits (1.5e-5 of the result on normal operands).  bias [N] and resid [M, N] may be NULL; out may be
- * resid itself at the same pitch.  ws: at least ff_gemm_q8_workspace_bytes(d) bytes (NULL if
- * that is 0; it is for most shapes: only few rows on a long K need one).
+ * sums over blocks in fp32, one rounding to out_dtype.  a_s w_s is formed first, in fp32: where that
+ * overflows, so does the result, or it is NaN.  Within a block, fp32 outputs take exact products
+ * summed in fp32; bf16 outputs take the 8-bit matrix instructions, which align a block's products
+ * to fewer bits: measured, off by at most 2^-11 of the block's largest |a| times its largest |w|
+ * (1.5e-5 of the result on normal operands, 5.5e-5 where exponents are spread widely).
+ * bias [N] and resid [M, N] may be NULL; out may be resid itself at the same pitch.  ws: at least
+ * ff_gemm_q8_workspace_bytes(d) bytes (NULL if that is 0; it is for most shapes: only few rows on a
+ * long K need one).
  * Errors: FF_E_NULL, FF_E_DTYPE, FF_E_RANGE (gelu), FF_E_SHAPE, FF_E_WORKSPACE, FF_E_HIP. */
 size_t ff_gemm_q8_workspace_bytes(const ff_gemm_q8_desc* d);   /* 0 also for an invalid descriptor */
 ff_status ff_gemm_q8(const ff_gemm_q8_desc* d, const void* a, const float* a_s, const void* w, const float* w_s,
@@ -509,18 +512,21 @@ ff_status ff_gemm_q8(const ff_gemm_q8_desc* d, const void* a, const float* a_s, 
  * (end = max(i + 1, prefix)), a window, the filled part of a cache, or the joint sequence
  * [txt ; img] with padded text (two spans).  A query with no key, or all of whose scores are
  * -inf, gets zeros.  What a key or value row holds (infinities, NaN) has no effect on a query
- * that does not see it.
+ * that does not see it; one that a query sees reaches its output, whatever its weight.
  * bias: FF_BIAS_NONE; FF_BIAS_SLOPE: - bias[h] |j - p_i|, fp32 [H]; FF_BIAS_TABLE:
  * bias[h][min(max(j - p_i, -R), R) + R], fp32 [H, 2 R + 1], R = bias_reach.  p_i = pos[b] + i, pos
  * int32 [B] (NULL: zeros; cut to +-2^30), is where query i stands among the keys.
- * Scores, statistics and sums are fp32; in bf16 the probabilities enter the product with v
- * rounded to bf16.  ws: at least ff_attention_workspace_bytes(d) bytes (NULL if that is 0:
- * only few queries on many keys, whose keys are split, need one). */
+ * Scores, statistics and sums are fp32; in bf16 the probabilities (relative to a running maximum,
+ * divided by their unrounded sum at the end) enter the product with v rounded to bf16.  Scores beyond
+ * 2^127 and values beyond 2^123 / n_k may overflow on the way.  ws: at least
+ * ff_attention_workspace_bytes(d) bytes (NULL if that is 0: only few queries on many keys, whose
+ * keys are split, need one). */
 enum { FF_BIAS_NONE = 0, FF_BIAS_SLOPE = 1, FF_BIAS_TABLE = 2 };
 
 /* B >= 1, H % H_kv == 0, d in [8, 128] and d % 8 == 0, n_q, n_k >= 0, n_q H B and n_k below 2^30,
- * B H_kv ceil(n_q (H / H_kv) / 16) below 2^23; strides non-negative multiples of 8, out's rows apart from each other; 64 key or value rows
- * within 2^31 bytes; scale in [2^-60, 2^60], cap 0 or in [2^-60, 2^60]; 0 <= bias_reach <= 2^20; n_spans 0, 1 or 2. */
+ * B H_kv ceil(n_q (H / H_kv) / 16) below 2^23; strides non-negative multiples of 8, out's rows
+ * apart from each other; 64 key or value rows within 2^31 bytes; scale in [2^-60, 2^60], cap 0 or in
+ * [2^-60, 2^60]; 0 <= bias_reach <= 2^20; n_spans 0, 1 or 2. */
 typedef struct {
   int32_t dtype, B, H, H_kv, d, n_q, n_k;
   int32_t bias_kind, bias_reach, n_spans;

@@ -182,7 +182,8 @@ __device__ __forceinline__ Place place_of(const AttnSpanArgs& a, int nsplit, int
   Place p;
   if (nsplit == 1) {
     // The last rows of all heads first, which see the most keys under a causal mask, so that short walks
-    // close the grid (fp32, 777 causal tokens, 24 heads of 64: 32.3 us; head after head 38.0)
+    // close the grid (fp32, heads of 64: B = 2, 12 heads, 777 causal tokens 33.8 us, head after head 39.4;
+    // 12 heads, 1500 tokens 51.4, 63.8)
     const int heads = a.B * a.H_kv;
     p.split = 0;
     p.tile = nt - 1 - id / heads;
@@ -464,8 +465,8 @@ __device__ __forceinline__ void attend16(const AttnSpanArgs& a, const Row& w, co
 // are split over workgroups too, in equal parts of the rows' own keys.
 // What bounds it: memory on long caches (B = 8 ragged up to 32768 keys, 16 heads on 4 of 128: 67 us and
 // 5 for the join, 4.5 TB/s), latency on short ones (33 tokens 6 us); in fp32 the fp32 MFMA rate and the
-// softmax's vector instructions, which do not run beside them (1500 tokens, 12 heads of 64: 92 us, 75
-// TFLOP/s; 32 rows a wavefront, with half the loads but two wavefronts a SIMD instead of three, 110).
+// softmax's vector instructions, which do not run beside them (1500 tokens, 12 heads of 64: 85 to 92 us, 75
+// to 82 TFLOP/s; 32 rows a wavefront, with half the loads but two wavefronts a SIMD instead of three, 110).
 template <int DT, int NE>
 __global__ __launch_bounds__(256, 2) void k_attn_dir(AttnSpanArgs a, int nsplit) {
 #ifdef __HIP_DEVICE_COMPILE__   // the host pass needs the launch stub only
@@ -602,8 +603,8 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnSpanArgs a, int nsplit, i
 // MOD: capped or biased scores, formed in log2 units before the softmax; caps above kFastCap have instances
 // of their own (with both in one, tanhf's constants took up to 6 registers of the others' loop, and
 // spilled 2 where there are 128).
-// What bounds it: as k_attn_pp, whose results it repeats bit for bit without spans, in its time (N =
-// 14566, H = 16, d = 128 1424 us).  With 256 of those rows padded text: 1400 to 1440 us, 1.18 PFLOP/s.  Short spans
+// What bounds it: as k_attn_pp, in its time (N = 14566, H = 16, d = 128 1424 us).  With 256 of those rows
+// padded text: 1390 to 1440 us, 1.16 to 1.2 PFLOP/s; 24 heads of 128, 8192 causal tokens 367 us, 1.12.  Short spans
 // are bound by what a workgroup does once, 8 us, and by the softmax of its partly seen tiles (packed prompts of
 // 4096 tokens with about 600 each, 16 heads on 8: 44 us, 180 TFLOP/s; capped 45 to 48).
 // (two workgroups share a CU where a K or V row takes 128 bytes of LDS: at most 128 VGPRs)
@@ -631,8 +632,11 @@ __global__ __launch_bounds__(512, RWB == 128 ? 4 : 2) void k_attn_span_pp(AttnSp
     const int nqb = (R + 128 * QT - 1) / (128 * QT), n = gridDim.x, id = blockIdx.x, heads = a.H_kv * a.B;
     // An XCD gets neighbouring places of one head after the other, the last rows first.  With spans its heads
     // go four at a time, the last rows of all four first (they see the most keys under a causal mask: 24
-    // heads of 128, 8192 tokens 270 us for 297; 24 of 64, 2048 tokens 51 for 63); heads that do not divide
-    // among the XCDs go all at once if they are few (20 of 128, 8000 tokens 232 us for 296).
+    // heads of 128, 8192 causal tokens 367 us for 416; 24 of 64, 2048 tokens 34 for 44); heads that do not
+    // divide among the XCDs go all at once if they are few (20 of 128, 8000 tokens 314 us for 391).  All at
+    // once, 33 to 60 heads would gain on causal masks too (33 of 128, 8000 tokens 520 us for 600), but 100
+    // would lose (8000 tokens 1632 us for 1522 to 1577), and so would heads whose rows all see as much (33 of
+    // 128, 14566 tokens, 256 of them padded: 3224 us for 2890 to 3000).
     int qr, bh;   // place from the last rows on, head of all samples
     if (a.n_spans && heads % 8 == 0) {
       const int i = id / 8, hx = heads / 8, first = i / (4 * nqb) * 4, m = min(4, hx - first), k = i - first * nqb;

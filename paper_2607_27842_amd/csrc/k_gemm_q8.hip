@@ -25,7 +25,7 @@ __device__ __forceinline__ i32x8_t join(u32x4_t lo, u32x4_t hi) {
 // fp32 outputs take exact products: e4m3 values widened to bf16 (exactly) on the bf16 MFMAs, whose
 // sums keep 24 bits (7.6e-8 of the result off on operands of widely spread exponents).  The 8-bit
 // MFMAs align a block's products to fewer bits (5.5e-5 off on the same operands, 1.5e-5 on normal
-// ones): far below a bf16 output's rounding of 2^-9, far above fp32's.
+// ones; a block's sum by at most 2^-11 of its largest |a| times its largest |w|, as measured): far below a bf16 output's rounding of 2^-9, far above fp32's.
 __device__ __forceinline__ bf16x8_t widen(uint32_t lo, uint32_t hi) {
   const bf16x2_t p[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true),
                          __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true)};
@@ -74,8 +74,10 @@ __device__ __forceinline__ void finish4(const GemmQ8Args& a, const Add4& x, int 
 }
 
 // Few rows: 16 x 16 tile, operands straight from memory, the NW waves of a workgroup on interleaved
-// blocks of K with the loads of four blocks in flight; their sums meet in LDS in wave order.  Bound
-// by the latency of that one round of loads: M = 1, N = 8192, K = 2048 5.7 us (16.8 MB of weights).
+// blocks of K; their sums meet in LDS in wave order.  Bound by the latency of the loads: M = 1, N = 8192,
+// K = 2048 6.2 us (16.8 MB of weights).  The compiler puts a block's loads behind the test that ends the
+// walk, so a wave has one block (four 16-byte loads) in flight, not the four that the loop requests, and
+// with bf16 outputs the first wave waits for bias and residual, which it widens at once.
 // Two or four 16-row tiles a workgroup, to read the weights once for them, were slower (M = 64, N =
 // 2048, K = 2048: 6.0 us against 7.1 with four): the rows come from the caches.
 template <int DT, int NW>
@@ -91,7 +93,7 @@ __global__ __launch_bounds__(NW * 64) void k_gemm_q8_dir(GemmQ8Args a) {
   const float* sa = a.a_s + m;
   const float* sw = a.w_s + (size_t)(n0 / kQBlock) * a.ws_ld;
   f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
-  // the first wave finishes the tile: what it adds is requested before the operands
+  // the first wave finishes the tile: what it adds is read before the operands
   const bool in = m0 + l16 < a.M && n0 + 4 * g < a.N;
   Add4 extra{acc, acc};
   if (wave == 0) extra = request4<DT>(a, in ? m0 + l16 : m0, in ? n0 + 4 * g : n0);
@@ -241,8 +243,10 @@ __device__ __forceinline__ void tile_at(int wg, int n, int tiles_m, int tiles_n,
 // The weight's scale of a stage is a scalar per wave (its columns lie in one block of 128).
 // K % 128 != 0: the last stage's chunks past K are out of the resource's range and load zeros.
 // What bounds it: with random operands the card's power limit in the main loop, then the epilogue, which
-// one workgroup a CU leaves uncovered.  M = 14566, N = 8192, K = 2048: 271 us (1.80 PFLOP/s; a library's
-// product with one scale a tensor takes 237), with GELU 294, with a residual 299.
+// one workgroup a CU leaves uncovered, and the last round of tiles.  M = 14566, N = 8192, K = 2048 (7.1 rounds
+// of 256 tiles, so 8): 248 to 271 us on different cards (1.8 to 2.0 PFLOP/s; a library's product with one
+// scale a tensor takes 241), on the first of them 273 with bias and GELU, 279 with bias and residual, and 233
+// for M = 14336, 7 rounds.
 constexpr int kPPIssue[4][3] = {{3, 8, -1}, {0, 4, 5}, {1, 6, -1}, {2, 7, -1}};   // A0-A3, B0-B3, scales
 // How many of a wave's DMAs may be outstanding at the end of phase p of a stage with `left` stages
 // after it (2: two or more), so that what phase p + 1 reads has landed.
@@ -759,7 +763,7 @@ long tiles(long M, long N, long t) { return ((M + t - 1) / t) * ((N + t - 1) / t
 //   N 8192 K 2048, M = 16: k_gemm_q8_dir 7.1 us against 8.0 with 64 x 64 tiles; M = 64: 17.8 against 8.1
 //   M 128 N 2048 K 8192: 64 x 64 tiles 17.7 us, with 2 / 4 / 8 splits 14.2 / 12.4 / 14.7
 //   M 512 N 8192 K 2048: 128 x 128 14.9 us, 64 x 64 20.9, 256 x 256 31.9
-//   M 14566 N 8192 K 2048: 256 x 256 263 us, 128 x 128 322, 64 x 64 444
+//   M 14566 N 8192 K 2048: 256 x 256 248 us, 128 x 128 315, 64 x 64 435 (fp32: 128 x 128 518, 64 x 64 649)
 Q8Plan gemm_q8_plan(int dt, int M, int N, int K) {
   const int nk = (K + kQBlock - 1) / kQBlock;
   // us per block of K: few tiles, what 256 tiles add, and a round of all CUs (512 tiles of 64 x 64)
@@ -793,7 +797,8 @@ hipError_t launch_q8(const GemmQ8Args& a, hipStream_t s) {
   const Q8Plan p = gemm_q8_plan(DT, a.M, a.N, a.K);
   switch (p.kernel) {
     case Q8_DIR: {
-      // 16 waves where 8 would take their blocks in two rounds on a part of the CUs
+      // 16 waves where 8 would take their blocks in two rounds on a part of the CUs (one row, K = 8192: N = 2048
+      // 7.8 us for 8.4; N = 8192, where all CUs are at work, 15.7 for 15.6)
       const long t = tiles(a.M, a.N, 16);
       if (a.K > 32 * kQBlock && t <= 256) FF_LAUNCH((k_gemm_q8_dir<DT, 16>), (unsigned)t, 1024, 0, s, a);
       else FF_LAUNCH((k_gemm_q8_dir<DT, 8>), (unsigned)t, 512, 0, s, a);

@@ -58,7 +58,7 @@ enum {
 };
 
 enum { FF_DIT = 0, FF_MMDIT_DOUBLE = 1, FF_MMDIT_SINGLE = 2 };          /* block kinds  */
-enum { FF_F32 = 0, FF_BF16 = 1 };                                        /* dtypes       */
+enum { FF_F32 = 0, FF_BF16 = 1, FF_I8 = 2 };   /* dtypes; FF_I8 only where a call names it */
 /* Modes (Sec. 3.3).  The last three are the matched-compute arms the paper weighs
  * whole-block forwarding against: forwarding the exact output on every part_stride-th
  * token (FF_TOKENS_PARTIAL) or channel (FF_CHANNELS_PARTIAL) only, and recomputing the
@@ -541,6 +541,103 @@ size_t ff_attention_workspace_bytes(const ff_attn_desc* d);   /* 0 also for an i
 ff_status ff_attention(const ff_attn_desc* d, const void* q, const void* k, const void* v, const float* bias,
                        const int32_t* pos, const int32_t* spans, void* out, void* ws, size_t ws_bytes,
                        ff_stream_t stream);
+
+/* ---------------------------------------------------------------- 8-bit integers
+ * Linears on 8-bit integers with a scale for each token and each output channel, and the step between two
+ * branches of a block (Eq. 1's backbones differ in both; the paper leaves them open, Sec. 3.1).  The rules
+ * of the 8-bit section above hold here too.  A row of 8-bit integers holds int8 values and one fp32 scale:
+ *     s = max(largest |v| of the row, 2^-100) (1 / 127),   q = the integer nearest v (1 / s),   v ~ s q,
+ * in fp32, ties to even, so that |q| <= 127.  A NaN or an infinity in a row makes its scale NaN and
+ * its integers zeros: no value of that row is taken for a number. */
+#define FF_I8_MAX_K 131056
+
+/* 0 <= rows <= 2^23, 8 <= C <= FF_I8_MAX_K, C % 8 == 0; x_row, q_row >= C and multiples of 8.  dtype: of x. */
+typedef struct {
+  int32_t rows, C, dtype;
+  int64_t x_row, q_row;
+} ff_quant_i8_desc;
+
+/* q [rows, C], s [rows] <- x [rows, C]: tokens, or the output channels of a weight [out, in], laid out once.
+ * Errors: FF_E_NULL, FF_E_DTYPE, FF_E_SHAPE (sizes, pitches, alignment, overlap), FF_E_HIP. */
+ff_status ff_quant_i8(const ff_quant_i8_desc* d, const void* x, void* q, float* s, ff_stream_t stream);
+
+/* 0 <= M <= 2^23, 8 <= N <= 2^20, N % 8 == 0, M N <= 2^34, 16 <= K <= FF_I8_MAX_K, K % 16 == 0; a_row, w_row >= K,
+ * multiples of 16 (a_row of 8 where A is not in 8 bits); out_row (and resid_row with resid) >= N, multiples of 8;
+ * 256 rows of 8-bit a or of w within 2^31 bytes.
+ * a_dtype: FF_I8, or FF_F32 / FF_BF16 for rows that the call puts in 8 bits as ff_quant_i8 does.
+ * out_dtype: of bias, resid and out. */
+typedef struct {
+  int32_t M, N, K, a_dtype, out_dtype;
+  int32_t gelu;           /* 1: GELU (tanh form) on the product with its bias, 0: none */
+  int32_t gate_rows;      /* with gate: row m takes gate vector m / gate_rows; >= 1 */
+  int64_t a_row, w_row, out_row, resid_row;
+  int64_t gate_ld;        /* with gate: between gate vectors, >= N and a multiple of 8, or 0 for one that all share */
+} ff_gemm_i8_desc;
+
+/* out [M, N] <- act(a_s[m] w_s[n] sum_k a[m, k] w[n, k] + bias[n]) gate[m / gate_rows][n] + resid[m, n]
+ * A [M, K] with scales a_s [M] (NULL unless a_dtype is FF_I8), W [N, K] int8 with w_s [N].  The sum is exact
+ * (integers below 2^31; values of -128 are taken as they are); then fp32, one rounding to out_dtype.  bias [N],
+ * gate (fp32 vectors of N: a block's per-sample gate) and resid [M, N] may be NULL; out may be resid
+ * itself at the same pitch.  ws: at least ff_gemm_i8_workspace_bytes(d) bytes (NULL if that is 0: it
+ * holds the rows that the call puts in 8 bits, and partial sums where few rows meet a long K).
+ * Errors: FF_E_NULL, FF_E_DTYPE, FF_E_RANGE (gelu, gate_rows), FF_E_SHAPE, FF_E_WORKSPACE, FF_E_HIP. */
+size_t ff_gemm_i8_workspace_bytes(const ff_gemm_i8_desc* d);   /* 0 also for an invalid descriptor */
+ff_status ff_gemm_i8(const ff_gemm_i8_desc* d, const void* a, const float* a_s, const void* w, const float* w_s,
+                     const void* bias, const float* gate, const void* resid, void* out, void* ws, size_t ws_bytes,
+                     ff_stream_t stream);
+
+enum { FF_NORM_NONE = 0, FF_NORM_RMS = 1, FF_NORM_LAYER = 2 };
+
+/* dtype: of x, branch, post_gain, pre_gain, sum and y.  0 <= rows <= 2^23, 8 <= C <= 16384, C % 8 == 0; the pitches of
+ * the tensors that are passed >= C and multiples of 8; eps > 0; resid_scale finite.
+ * mod_rows (>= 1 with gate, scale or shift): row r takes vector r / mod_rows, one a sample; gate_ld, mod_ld: between
+ * gate vectors, and between scale and shift vectors, >= C and multiples of 8, or 0 for one that all rows share. */
+typedef struct {
+  int32_t rows, C, dtype;
+  int32_t post, pre;      /* FF_NORM_*: behind the branch, in front of the next one */
+  int32_t gate_tanh;      /* 1: tanh of the gate */
+  int32_t mod_rows;
+  float eps, resid_scale;
+  int64_t x_row, branch_row, sum_row, y_row, q_row, gate_ld, mod_ld;
+} ff_branch_norm_desc;
+
+/* What stands between two branches of a block, on rows [rows, C]:
+ *     t = round_dtype(resid_scale x + g N_post(branch) post_gain),   g = gate or tanh(gate)
+ *     v = N_pre(t) pre_gain (1 + scale) + shift
+ * N: v / sqrt(mean(v^2) + eps) (FF_NORM_RMS), that of v less its mean (FF_NORM_LAYER), or v (FF_NORM_NONE); fp32.
+ * branch (and post_gain, gate) NULL: t = round_dtype(resid_scale x).  The gains [C], gate, scale and shift (fp32
+ * vectors of C) may be NULL: ones, and zeros for scale and shift.  sum (may be x or branch itself, at the same pitch)
+ * receives t, y v rounded to dtype, q with q_s (NULL together) v as rows of 8-bit integers, from the
+ * unrounded v; each may be NULL, but not all.
+ * Errors: FF_E_NULL, FF_E_DTYPE, FF_E_RANGE (post, pre, gate_tanh, mod_rows, eps, resid_scale), FF_E_SHAPE, FF_E_HIP. */
+ff_status ff_branch_norm_i8(const ff_branch_norm_desc* d, const void* x, const void* branch, const void* post_gain,
+                            const float* gate, const void* pre_gain, const float* scale, const float* shift, void* sum,
+                            void* y, void* q, float* q_s, ff_stream_t stream);
+
+/* ---------------------------------------------------------------- 8-bit history
+ * The feature history (Eq. 2) at half the bytes of bf16: int8 values with an fp32 scale for each block of 128, by the
+ * formula above with a block for a row.  A sample's N*C values, in order, make ceil(N*C / 128) blocks, the last one
+ * padded with zeros; a NaN or an infinity makes its block's values NaN.  A cache of n_slots slots per layer is
+ * [L][n_slots] slots of
+ *     int8 [B][blocks][128], then fp32 [B][blocks], then up to the next multiple of 128 bytes,
+ * in the caller's memory, apart from the cache that a context uses.
+ * ff_cache_i8_bytes: its bytes (0 for an invalid descriptor).
+ * ff_cache_update_i8, ff_draft_forecast_i8, ff_verify_replace_i8: as the calls without _i8, on such a
+ * cache.  The update puts the unrounded fp32 difference h - u (or h) in 8 bits; the draft and the
+ * verify pass sum coeffs[m] (s q) in fp32.  Outputs overlap neither the cache nor, unless they are u itself, u;
+ * ws and rel_l1 overlap nothing.
+ * Errors: as the calls without _i8. */
+#define FF_I8_BLOCK 128
+size_t ff_cache_i8_bytes(const ff_model_desc* m, int32_t n_slots);
+ff_status ff_cache_update_i8(const ff_model_desc* m, void* cache, int32_t n_slots, int32_t layer, int32_t slot,
+                             const void* u, const void* h, int32_t feature_mode, ff_stream_t stream);
+ff_status ff_draft_forecast_i8(const ff_model_desc* m, const void* cache, int32_t n_slots, int32_t layer,
+                               int32_t k_eff, const int32_t* slots, const float* coeffs, const void* u, void* h_d,
+                               ff_stream_t stream);
+ff_status ff_verify_replace_i8(const ff_model_desc* m, const void* cache, int32_t n_slots, int32_t layer,
+                               int32_t k_eff, const int32_t* slots, const float* coeffs, const void* u,
+                               const void* h_f, void* h_out, int32_t forward, int32_t stride, float eps,
+                               float* rel_l1, void* ws, size_t ws_bytes, ff_stream_t stream);
 
 /* ---------------------------------------------------------------- profiling
  * Optional tracing of a context's launches (Sec. 4 reports latency per arm; this

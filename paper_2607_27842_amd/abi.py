@@ -18,7 +18,7 @@ FF_OK, FF_E_NULL, FF_E_SHAPE, FF_E_DTYPE, FF_E_RANGE, FF_E_STATE, FF_E_WORKSPACE
     FF_E_UNSUPPORTED = 0, -1, -2, -3, -4, -5, -6, -7, -8
 FF_DIT, FF_MMDIT_DOUBLE, FF_MMDIT_SINGLE = 0, 1, 2
 FF_ABI_VERSION = 3          # the struct layouts below; must equal the library's
-FF_F32, FF_BF16 = 0, 1
+FF_F32, FF_BF16, FF_I8 = 0, 1, 2
 FF_VANILLA, FF_DRAFT, FF_VERIFY, FF_FEATFIX, FF_EXACT_ONLY = 0, 1, 2, 3, 4
 FF_TOKENS_PARTIAL, FF_CHANNELS_PARTIAL, FF_RECOMPUTE = 5, 6, 7
 FF_FWD_DRAFT, FF_FWD_EXACT, FF_FWD_TOKENS, FF_FWD_CHANNELS = 0, 1, 2, 3
@@ -28,6 +28,8 @@ FF_ACT_EXACT, FF_ACT_DRAFT, FF_ACT_SITE, FF_ACT_RECOMPUTE = 0, 1, 2, 3
 FF_MAX_K, FF_MAX_SLOTS, FF_TEMB_DIM = 3, 8, 256
 FF_NOALLOC_VERIFY_MAX_B = 16
 FF_Q8_BLOCK = 128
+FF_I8_BLOCK, FF_I8_MAX_K = 128, 131056
+FF_NORM_NONE, FF_NORM_RMS, FF_NORM_LAYER = 0, 1, 2
 FF_BIAS_NONE, FF_BIAS_SLOPE, FF_BIAS_TABLE = 0, 1, 2
 
 # every symbol include/featfix.h declares
@@ -37,6 +39,8 @@ EXPORTED = ("ff_abi_version", "ff_last_error", "ff_plan_build", "ff_plan_destroy
             "ff_ctx_reset", "ff_get_counts", "ff_ctx_step_kinds", "ff_denoise_step", "ff_ctx_trace", "ff_hist_sum_bytes", "ff_ctx_hist_sums", "ff_cond_cache_bytes", "ff_ctx_cond_cache", "ff_rel_l1",
             "ff_quant_q8", "ff_rms_norm_q8", "ff_gemm_q8_workspace_bytes", "ff_gemm_q8",
             "ff_attention_workspace_bytes", "ff_attention",
+            "ff_quant_i8", "ff_gemm_i8_workspace_bytes", "ff_gemm_i8", "ff_branch_norm_i8",
+            "ff_cache_i8_bytes", "ff_cache_update_i8", "ff_draft_forecast_i8", "ff_verify_replace_i8",
             "ff_ctx_profile", "ff_ctx_profile_read")
 PROF_CLASSES = ("gemm", "attn", "norm", "gemv", "draft", "verify", "cache", "other")
 
@@ -98,6 +102,23 @@ class ff_norm_desc(C.Structure):
 class ff_gemm_q8_desc(C.Structure):
     _fields_ = [(f, C.c_int32) for f in ("M", "N", "K", "out_dtype", "gelu")] + \
                [(f, C.c_int64) for f in ("a_row", "w_row", "out_row", "resid_row", "as_ld", "ws_ld")]
+
+
+class ff_quant_i8_desc(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("C", C.c_int32), ("dtype", C.c_int32), ("x_row", C.c_int64), ("q_row", C.c_int64)]
+
+
+class ff_gemm_i8_desc(C.Structure):
+    _fields_ = [("M", C.c_int32), ("N", C.c_int32), ("K", C.c_int32), ("a_dtype", C.c_int32), ("out_dtype", C.c_int32),
+                ("gelu", C.c_int32), ("gate_rows", C.c_int32),
+                ("a_row", C.c_int64), ("w_row", C.c_int64), ("out_row", C.c_int64), ("resid_row", C.c_int64), ("gate_ld", C.c_int64)]
+
+
+class ff_branch_norm_desc(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("C", C.c_int32), ("dtype", C.c_int32), ("post", C.c_int32), ("pre", C.c_int32),
+                ("gate_tanh", C.c_int32), ("mod_rows", C.c_int32), ("eps", C.c_float), ("resid_scale", C.c_float),
+                ("x_row", C.c_int64), ("branch_row", C.c_int64), ("sum_row", C.c_int64), ("y_row", C.c_int64),
+                ("q_row", C.c_int64), ("gate_ld", C.c_int64), ("mod_ld", C.c_int64)]
 
 
 class ff_attn_desc(C.Structure):
@@ -164,6 +185,15 @@ def lib():
             "ff_gemm_q8": (i32, [P(ff_gemm_q8_desc)] + [vp] * 8 + [sz, vp]),
             "ff_attention_workspace_bytes": (sz, [P(ff_attn_desc)]),
             "ff_attention": (i32, [P(ff_attn_desc)] + [vp] * 8 + [sz, vp]),
+            "ff_quant_i8": (i32, [P(ff_quant_i8_desc), vp, vp, vp, vp]),
+            "ff_gemm_i8_workspace_bytes": (sz, [P(ff_gemm_i8_desc)]),
+            "ff_gemm_i8": (i32, [P(ff_gemm_i8_desc)] + [vp] * 9 + [sz, vp]),
+            "ff_branch_norm_i8": (i32, [P(ff_branch_norm_desc)] + [vp] * 12),
+            "ff_cache_i8_bytes": (sz, [P(ff_model_desc), i32]),
+            "ff_cache_update_i8": (i32, [P(ff_model_desc), vp, i32, i32, i32, vp, vp, i32, vp]),
+            "ff_draft_forecast_i8": (i32, [P(ff_model_desc), vp, i32, i32, i32, P(i32), P(C.c_float), vp, vp, vp]),
+            "ff_verify_replace_i8": (i32, [P(ff_model_desc), vp, i32, i32, i32, P(i32), P(C.c_float), vp, vp, vp,
+                                           i32, i32, f32, vp, vp, sz, vp]),
             "ff_ctx_profile": (i32, [vp, i32]),
             "ff_ctx_profile_read": (i32, [vp, P(ff_prof_stat)]),
         }
@@ -355,6 +385,47 @@ def ff_attention_workspace_bytes(desc):
 def ff_attention(desc, q, k, v, bias, pos, spans, out, ws, ws_bytes, stream=0):
     """Attention of each query over its spans of keys; ws of ff_attention_workspace_bytes(desc)."""
     return check(lib().ff_attention(C.byref(desc), q, k, v, bias, pos, spans, out, ws, ws_bytes, stream))
+
+
+# Operators on 8-bit integers, and the step between two branches of a block.
+def ff_quant_i8(desc, x, q, s, stream=0):
+    """q, s <- rows of x in 8-bit integers with a scale a row."""
+    return check(lib().ff_quant_i8(C.byref(desc), x, q, s, stream))
+
+
+def ff_gemm_i8_workspace_bytes(desc):
+    return lib().ff_gemm_i8_workspace_bytes(C.byref(desc))
+
+
+def ff_gemm_i8(desc, a, a_s, w, w_s, bias, gate, resid, out, ws, ws_bytes, stream=0):
+    """out <- act(A W^T + bias) gate + resid on 8-bit integers; ws of ff_gemm_i8_workspace_bytes(desc)."""
+    return check(lib().ff_gemm_i8(C.byref(desc), a, a_s, w, w_s, bias, gate, resid, out, ws, ws_bytes, stream))
+
+
+def ff_branch_norm_i8(desc, x, branch, post_gain, gate, pre_gain, scale, shift, sum, y, q, q_s, stream=0):
+    """sum <- the scaled residual and the gated, normed branch; y and q, q_s <- its norm with scale and shift."""
+    return check(lib().ff_branch_norm_i8(C.byref(desc), x, branch, post_gain, gate, pre_gain, scale, shift, sum, y, q, q_s, stream))
+
+
+def ff_cache_i8_bytes(model, n_slots):
+    return lib().ff_cache_i8_bytes(C.byref(model), n_slots)
+
+
+def ff_cache_update_i8(model, cache, n_slots, layer, slot, u, h, feature_mode=FF_RESIDUAL, stream=0):
+    return check(lib().ff_cache_update_i8(C.byref(model), cache, n_slots, layer, slot, u, h, feature_mode, stream))
+
+
+def ff_draft_forecast_i8(model, cache, n_slots, layer, k_eff, slots, coeffs, u, h_d, stream=0):
+    return check(lib().ff_draft_forecast_i8(C.byref(model), cache, n_slots, layer, k_eff, _i32arr(slots),
+                                            _f32arr(coeffs), u, h_d, stream))
+
+
+def ff_verify_replace_i8(model, cache, n_slots, layer, k_eff, slots, coeffs, u, h_f, h_out, forward, eps,
+                         rel_l1, ws, ws_bytes, stream=0, stride=1):
+    """ff_verify_replace on the 8-bit history."""
+    return check(lib().ff_verify_replace_i8(C.byref(model), cache, n_slots, layer, k_eff, _i32arr(slots),
+                                            _f32arr(coeffs), u, h_f, h_out, int(forward), int(stride), eps, rel_l1,
+                                            ws, ws_bytes, stream))
 
 
 def ff_ctx_profile(ctx, enable):

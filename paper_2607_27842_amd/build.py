@@ -18,7 +18,7 @@ LIB = os.path.join(PKG, "libfeatfix.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 SOURCES = ["featfix.cpp", "k_mem.hip", "k_misc.hip", "k_gemm.hip", "k_attn.hip", "operators.cpp", "k_q8.hip", "k_gemm_q8.hip",
-           "k_attn_span.hip"]
+           "k_attn_span.hip", "k_i8.hip", "k_gemm_i8.hip", "k_mem_i8.hip"]
 FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-I", INCLUDE, "-I", CSRC,
          # packed fp32 instructions stay off: hipcc would otherwise form them from float code
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

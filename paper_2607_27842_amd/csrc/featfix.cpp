@@ -806,6 +806,35 @@ ff_status check_verify(const ff_model_desc* m, const void* cache, int32_t n_slot
   return FF_OK;
 }
 
+// The 8-bit history: a slot's place, the terms of a draft, and outputs that would meet what the call reads.
+uint8_t* i8_slot(const Model& m, const void* cache, int n_slots, int layer, int slot) {
+  return const_cast<uint8_t*>(static_cast<const uint8_t*>(cache)) + ((size_t)layer * n_slots + slot) * i8_slot_bytes(m.B, (size_t)m.N * m.C);
+}
+float* i8_scales(const Model& m, uint8_t* slot) { return reinterpret_cast<float*>(slot + m.B * i8_blocks((size_t)m.N * m.C) * kI8Block); }
+bool meets(const void* a, size_t an, const void* b, size_t bn) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return a && b && x < y + bn && y < x + an;
+}
+
+ff_status check_terms_i8(const Model& m, int n_slots, int layer, int k_eff, const int32_t* slots, const float* coeffs,
+                         const void* cache, const void* u, const void* out, TermsI8* t) {
+  Terms plain{};
+  const ff_status e = check_terms(m, n_slots, layer, k_eff, slots, coeffs, cache, &plain);
+  if (e) return e;
+  const size_t tb = m.E() * m.es();
+  if (out != u && meets(out, tb, u, tb)) return fail(FF_E_SHAPE, "the output overlaps u without being u");
+  if (meets(out, tb, cache, (size_t)m.L * n_slots * i8_slot_bytes(m.B, (size_t)m.N * m.C)))
+    return fail(FF_E_SHAPE, "the output overlaps the cache");
+  t->n = plain.n;
+  for (int q = 0; q < kMaxTerms; ++q) {
+    uint8_t* const at = q < plain.n ? i8_slot(m, cache, n_slots, layer, slots[q]) : nullptr;
+    t->slot[q] = at;
+    t->scales[q] = at ? i8_scales(m, at) : nullptr;
+    t->c[q] = plain.c[q];
+  }
+  return FF_OK;
+}
+
 // Partial sums of ff_verify_replace_noalloc: a fixed device array per GPU (each device
 // that loads the library holds its own copy until the process ends).  Host code never
 // uses the array's name as an address: the address of the current device's copy comes
@@ -986,6 +1015,92 @@ ff_status ff_verify_replace_noalloc(const ff_model_desc* m, const void* cache, i
     const Forward fw{forward, stride, md.C};
     HIP_TRY(ff::verify(md.dtype, t, u, h_f, h_out, fw, md.B, (size_t)md.N * md.C, eps, rel_l1, part,
                        reinterpret_cast<hipStream_t>(stream)), "verify (no allocation)");
+    return ok();
+  } catch (...) {
+    return fail(FF_E_UNSUPPORTED, "unexpected host exception");
+  }
+}
+
+size_t ff_cache_i8_bytes(const ff_model_desc* m, int32_t n_slots) {
+  try {
+    Model md;
+    if (check_model(m, &md) != FF_OK || n_slots < 1) return 0;
+    return (size_t)md.L * n_slots * i8_slot_bytes(md.B, (size_t)md.N * md.C);
+  } catch (...) {
+    return 0;
+  }
+}
+
+ff_status ff_cache_update_i8(const ff_model_desc* m, void* cache, int32_t n_slots, int32_t layer, int32_t slot, const void* u,
+                             const void* h, int32_t feature_mode, ff_stream_t stream) {
+  try {
+    Model md;
+    const ff_status e = check_model(m, &md);
+    if (e) return e;
+    if (!cache || !h) return fail(FF_E_NULL, "cache or h is NULL");
+    if (feature_mode != FF_RESIDUAL && feature_mode != FF_OUTPUT) return fail(FF_E_RANGE, "feature_mode unknown");
+    if (feature_mode == FF_RESIDUAL && !u) return fail(FF_E_NULL, "u is NULL in residual mode");
+    if (layer < 0 || layer >= md.L) return fail(FF_E_RANGE, "layer %d out of range", layer);
+    if (n_slots < 1 || n_slots > FF_MAX_SLOTS || slot < 0 || slot >= n_slots)
+      return fail(FF_E_RANGE, "slot %d / n_slots %d out of range", slot, n_slots);
+    const void* const from = feature_mode == FF_RESIDUAL ? u : nullptr;
+    if (!aligned16(cache) || !aligned16(h) || (from && !aligned16(from))) return fail(FF_E_SHAPE, "pointers must be 16-byte aligned");
+    const size_t n = (size_t)md.N * md.C, tb = md.E() * md.es();
+    uint8_t* const at = i8_slot(md, cache, n_slots, layer, slot);
+    if (meets(at, i8_slot_bytes(md.B, n), h, tb) || meets(at, i8_slot_bytes(md.B, n), from, tb))
+      return fail(FF_E_SHAPE, "the slot overlaps u or h");
+    HIP_TRY(ff::cache_update_i8(md.dtype, at, i8_scales(md, at), from, h, md.B, n, reinterpret_cast<hipStream_t>(stream)),
+            "8-bit cache update");
+    return ok();
+  } catch (...) {
+    return fail(FF_E_UNSUPPORTED, "unexpected host exception");
+  }
+}
+
+ff_status ff_draft_forecast_i8(const ff_model_desc* m, const void* cache, int32_t n_slots, int32_t layer, int32_t k_eff,
+                               const int32_t* slots, const float* coeffs, const void* u, void* h_d, ff_stream_t stream) {
+  try {
+    Model md;
+    ff_status e = check_model(m, &md);
+    if (e) return e;
+    if (!h_d) return fail(FF_E_NULL, "h_d is NULL");
+    if (!aligned16(h_d) || (u && !aligned16(u))) return fail(FF_E_SHAPE, "pointers must be 16-byte aligned");
+    TermsI8 t{};
+    e = check_terms_i8(md, n_slots, layer, k_eff, slots, coeffs, cache, u, h_d, &t);
+    if (e) return e;
+    HIP_TRY(ff::draft_i8(md.dtype, t, u, h_d, md.B, (size_t)md.N * md.C, reinterpret_cast<hipStream_t>(stream)), "draft (8-bit history)");
+    return ok();
+  } catch (...) {
+    return fail(FF_E_UNSUPPORTED, "unexpected host exception");
+  }
+}
+
+ff_status ff_verify_replace_i8(const ff_model_desc* m, const void* cache, int32_t n_slots, int32_t layer, int32_t k_eff,
+                               const int32_t* slots, const float* coeffs, const void* u, const void* h_f, void* h_out,
+                               int32_t forward, int32_t stride, float eps, float* rel_l1, void* ws, size_t ws_bytes,
+                               ff_stream_t stream) {
+  try {
+    Model md;
+    Terms plain{};
+    TermsI8 t{};
+    ff_status e = check_verify(m, cache, n_slots, layer, k_eff, slots, coeffs, u, h_f, h_out, forward, stride, eps, &md, &plain);
+    if (e) return e;
+    if (!ws) return fail(FF_E_NULL, "ws is NULL");
+    e = check_terms_i8(md, n_slots, layer, k_eff, slots, coeffs, cache, u, h_out, &t);
+    if (e) return e;
+    const Ws L = ws_layout(md);
+    if (ws_bytes < L.total) return fail(FF_E_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, L.total);
+    const size_t tb = md.E() * md.es(), rb = (size_t)md.B * 4;
+    if (!aligned16(ws) || ((uintptr_t)rel_l1 & 3u)) return fail(FF_E_SHAPE, "ws must be 16-byte aligned, rel_l1 4-byte aligned");
+    const void* const held[] = {u, h_f, h_out};
+    for (const void* p : held)
+      if (meets(ws, L.total, p, tb) || meets(rel_l1, rb, p, tb)) return fail(FF_E_SHAPE, "ws or rel_l1 overlaps a tensor");
+    if (meets(rel_l1, rb, ws, L.total)) return fail(FF_E_SHAPE, "rel_l1 overlaps ws");
+    const size_t cb = (size_t)md.L * n_slots * i8_slot_bytes(md.B, (size_t)md.N * md.C);
+    if (meets(ws, L.total, cache, cb) || meets(rel_l1, rb, cache, cb)) return fail(FF_E_SHAPE, "ws or rel_l1 overlaps the cache");
+    const Forward fw{forward, stride, md.C};
+    HIP_TRY(ff::verify_i8(md.dtype, t, u, h_f, h_out, fw, md.B, (size_t)md.N * md.C, eps, rel_l1, at<float>(ws, L.PART),
+                          reinterpret_cast<hipStream_t>(stream)), "verify (8-bit history)");
     return ok();
   } catch (...) {
     return fail(FF_E_UNSUPPORTED, "unexpected host exception");

@@ -6,7 +6,7 @@
 // columns 4 (l / 16) + 0..3.  Lane l of an operand takes row l % 16 and two 16-byte chunks of the
 // block, chunks l / 16 and 4 + l / 16; which k stands where within the block does not matter as
 // long as both operands agree.
-#include "dev_common.h"
+#include "gemm_8bit.h"
 #include <math.h>
 
 namespace ff {
@@ -47,12 +47,6 @@ __device__ __forceinline__ f32x4_t product(u32x4_t w0, u32x4_t w1, u32x4_t x0, u
 // 4 consecutive columns c.. of output row r (N % 8 == 0: in range as a whole): what is added to the
 // product, and the rest of the epilogue
 struct Add4 { f32x4_t bias, resid; };
-template <int DT>
-__device__ __forceinline__ f32x4_t load4(const void* p, size_t i) {
-  if (DT == DT_F32) return *reinterpret_cast<const f32x4_t*>(reinterpret_cast<const float*>(p) + i);
-  const u32x2_t w = *reinterpret_cast<const u32x2_t*>(reinterpret_cast<const uint16_t*>(p) + i);
-  return f32x4_t{__uint_as_float(w[0] << 16), __uint_as_float(w[0] & 0xffff0000u), __uint_as_float(w[1] << 16), __uint_as_float(w[1] & 0xffff0000u)};
-}
 template <int DT>
 __device__ __forceinline__ Add4 request4(const GemmQ8Args& a, int r, int c) {
   Add4 x{{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
@@ -142,28 +136,6 @@ __global__ __launch_bounds__(NW * 64) void k_gemm_q8_dir(GemmQ8Args a) {
   if (in) finish4<DT>(a, extra, m0 + l16, n0 + 4 * g, acc);
 }
 
-// 8 values as they are stored, to be added later
-template <int DT> struct Raw8;
-template <> struct Raw8<DT_BF16> {
-  typedef u32x4_t type;
-  __device__ __forceinline__ static type load(const void* p, size_t i) { return *reinterpret_cast<const u32x4_t*>(reinterpret_cast<const uint16_t*>(p) + i); }
-  __device__ __forceinline__ static void add(type w, float* v) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] += __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
-  }
-};
-template <> struct Raw8<DT_F32> {
-  struct type { f32x4_t x[2]; };
-  __device__ __forceinline__ static type load(const void* p, size_t i) {
-    const f32x4_t* q = reinterpret_cast<const f32x4_t*>(reinterpret_cast<const float*>(p) + i);
-    return type{{q[0], q[1]}};
-  }
-  __device__ __forceinline__ static void add(const type& w, float* v) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] += w.x[e / 4][e % 4];
-  }
-};
-
 // Epilogue of a wavefront's 16 TM x 16 TN block at (r0, c0), acc in the MFMA layout (lane l: row l % 16
 // of each 16, columns 4 (l / 16) + 0..3): 32 rows at a time go through the wave's own LDS region as
 // fp32 rows and come back as 8-column pieces, so that every load and store of bias, residual and
@@ -215,16 +187,6 @@ __device__ __forceinline__ void epilogue(const GemmQ8Args& a, int r0, int c0, co
       if (r < a.M && c < a.N) store8<DT>(a.out, (size_t)r * a.out_row + c, v);
     }
   }
-}
-
-// Workgroup -> tile: workgroups go round-robin over the 8 XCDs, so every XCD gets a contiguous range
-// of tiles, in groups of 8 tile rows, whose operand rows its L2 then shares.
-__device__ __forceinline__ void tile_at(int wg, int n, int tiles_m, int tiles_n, int& tm, int& tn) {
-  const int full = n / 8 * 8;
-  const int id = wg < full ? (wg % 8) * (full / 8) + wg / 8 : wg;
-  const int per = 8 * tiles_n, first = id / per * 8, size = min(tiles_m - first, 8), in = id % per;
-  tm = __builtin_amdgcn_readfirstlane(first + in % size);
-  tn = __builtin_amdgcn_readfirstlane(in / size);
 }
 
 // ---------------------------------------------------------------- large grids: two wave groups in turn

@@ -373,6 +373,11 @@ hipError_t rel_l1(int dtype, const void* a, const void* b, int B, size_t Eb, flo
   return hipGetLastError();
 }
 
+hipError_t verify_finish(const float* partials, int B, int groups, float eps, float* rel, hipStream_t s) {
+  FF_LAUNCH(k_verify_finish, dim3(B), kThreads, 0, s, partials, groups, eps, rel);
+  return hipGetLastError();
+}
+
 hipError_t copy_rows(int dtype, const void* src, void* dst, int B, int n, int N, int off, int C, hipStream_t st) {
   const int V = dtype == DT_BF16 ? 8 : 4;
   size_t nchunk = (size_t)B * n * (C / V);

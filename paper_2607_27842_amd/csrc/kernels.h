@@ -182,6 +182,51 @@ Q8Plan gemm_q8_plan(int out_dtype, int M, int N, int K);
 size_t gemm_q8_workspace(int out_dtype, int M, int N, int K);
 hipError_t gemm_q8(int out_dtype, const GemmQ8Args& a, hipStream_t s);
 
+// ---------------------------------------------------------------- 8-bit integers
+// Values as signed bytes with an fp32 scale per row, or in the history per block of 128; include/featfix.h states
+// the format.
+struct QuantI8Args {
+  const void* x; int64_t x_row;
+  uint8_t* q; int64_t q_row;
+  float* s;
+  int rows, C;
+};
+hipError_t quant_i8(int dtype, const QuantI8Args& a, hipStream_t s);
+// t = round(resid_scale x + gate N_post(branch) post_gain), v = N_pre(t) pre_gain (1 + scale) + shift; sum <- t,
+// y <- v, q and q_s <- v in 8 bits (each where not NULL).  Row r takes row r / mod_rows of gate, scale, shift.
+enum { NORM_NONE = 0, NORM_RMS = 1, NORM_LAYER = 2 };
+struct BranchArgs {
+  const void* x; int64_t x_row;
+  const void* branch; int64_t branch_row;
+  const void *post_gain, *pre_gain;
+  const float* gate; int64_t gate_ld;
+  const float *scale, *shift; int64_t mod_ld;
+  void* sum; int64_t sum_row;
+  void* y; int64_t y_row;
+  uint8_t* q; int64_t q_row; float* q_s;
+  int rows, C, post, pre, gate_tanh, mod_rows;
+  float eps, resid_scale;
+};
+hipError_t branch_norm(int dtype, const BranchArgs& a, hipStream_t s);
+// out = act(a_s[m] w_s[n] sum_k a[m, k] w[n, k] + bias) gate[m / gate_rows] + resid
+struct GemmI8Args {
+  const void* a; int64_t a_row; const float* a_s;   // bytes and their scales, or rows of a_dtype and NULL
+  const uint8_t* w; int64_t w_row; const float* w_s;
+  const void* bias; const void* resid; int64_t resid_row;   // in the output's type
+  const float* gate; int64_t gate_ld; int gate_rows;
+  void* out; int64_t out_row;
+  int M, N, K, gelu;
+  int* part;   // workspace: gemm_i8_workspace bytes
+};
+constexpr int kI8MaxK = 131056;   // K * 128 * 128 < 2^31: sums of products stay within 32 bits
+enum { DT_I8 = 2 };
+// What a shape is run with: a kernel (its tile), and workgroups that share a tile's K
+enum { I8_DIR, I8_TILE64, I8_TILE128, I8_TILE256 };
+struct I8Plan { int kernel, splits; };
+I8Plan gemm_i8_plan(int a_dtype, int out_dtype, int M, int N, int K);
+size_t gemm_i8_workspace(int a_dtype, int out_dtype, int M, int N, int K);
+hipError_t gemm_i8(int a_dtype, int out_dtype, const GemmI8Args& a, hipStream_t s);
+
 // ---------------------------------------------------------------- attention over spans
 // Rows of a (sample, key head): row r is query r / G of query head hk * G + r % G.
 enum { BIAS_NONE = 0, BIAS_SLOPE = 1, BIAS_TABLE = 2 };
@@ -231,6 +276,25 @@ hipError_t verify(int dtype, const Terms& t, const void* u, const void* hf, void
 // two-stage reduction; partials as for verify)
 hipError_t rel_l1(int dtype, const void* a, const void* b, int B, size_t Eb, float eps, float* rel, float* partials,
                   hipStream_t s);
+
+// rel[b] from groups partial sums per sample, as verify and rel_l1 write them
+hipError_t verify_finish(const float* partials, int B, int groups, float eps, float* rel, hipStream_t s);
+
+// The history in 8-bit integers: blocks of 128 values of a sample's n (a multiple of 8), the last one padded.  A slot
+// holds [B, blocks, 128] bytes, then [B, blocks] scales.
+constexpr int kI8Block = 128;
+inline size_t i8_blocks(size_t n) { return (n + kI8Block - 1) / kI8Block; }
+inline size_t i8_slot_bytes(int B, size_t n) { return (B * i8_blocks(n) * (kI8Block + 4) + 127) / 128 * 128; }
+struct TermsI8 {
+  int n;
+  const uint8_t* slot[kMaxTerms];
+  const float* scales[kMaxTerms];
+  float c[kMaxTerms];
+};
+hipError_t cache_update_i8(int dtype, uint8_t* slot, float* scales, const void* u, const void* h, int B, size_t n, hipStream_t s);
+hipError_t draft_i8(int dtype, const TermsI8& t, const void* u, void* hd, int B, size_t n, hipStream_t s);
+hipError_t verify_i8(int dtype, const TermsI8& t, const void* u, const void* hf, void* hout, const Forward& fw, int B, size_t n,
+                     float eps, float* rel, float* partials, hipStream_t s);
 
 // ---------------------------------------------------------------- small per-step kernels
 // phi[k] = cos(s f_k), phi[128 + k] = sin(s f_k), f_k = exp(-ln(1e4) k / 128), in fp64.

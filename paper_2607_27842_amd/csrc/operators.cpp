@@ -1,5 +1,5 @@
-// Host side of the operators on 8-bit operands and of attention over spans: argument checks and
-// dispatch behind include/featfix.h.  Everything is checked before anything is launched.
+// Host side of the operators on 8-bit operands, between branches and of attention over spans: argument
+// checks and dispatch behind include/featfix.h.  Everything is checked before anything is launched.
 #include <math.h>
 
 #include "featfix.h"
@@ -88,6 +88,64 @@ ff_status check_gemm(const ff_gemm_q8_desc* d, bool resid) {
   CHECK(d->as_ld <= kMaxPitch && d->ws_ld <= kMaxPitch && (wide)256 * d->a_row < lim && (wide)256 * d->w_row < lim &&
         (wide)nb * d->as_ld * 4 < lim && (wide)na * d->ws_ld * 4 < lim, FF_E_SHAPE,
         "256 operand rows and the scales of an operand must lie within 2^31 bytes");
+  return FF_OK;
+}
+
+ff_status check_quant_i8(const ff_quant_i8_desc* d) {
+  CHECK(d, FF_E_NULL, "quant descriptor is NULL");
+  CHECK(dtype_ok(d->dtype), FF_E_DTYPE, "unknown dtype %d", d->dtype);
+  CHECK(d->rows >= 0 && d->rows <= kMaxRows, FF_E_SHAPE, "rows=%d outside [0, 2^23]", d->rows);
+  CHECK(d->C >= 8 && d->C % 8 == 0 && d->C <= kI8MaxK, FF_E_SHAPE, "C=%d must be a multiple of 8 in [8, %d]", d->C, kI8MaxK);
+  CHECK(pitch_ok(d->x_row, d->C, 8) && pitch_ok(d->q_row, d->C, 8), FF_E_SHAPE, "x_row and q_row must be multiples of 8 and >= C");
+  return FF_OK;
+}
+
+// vectors of `cols` fp32 values, one a group of rows: pitch 0 for one vector that all groups share
+bool vectors_ok(int64_t ld, int64_t cols) { return ld == 0 || pitch_ok(ld, cols, 8); }
+Extent vectors_of(const void* p, int64_t rows, int64_t per, int64_t cols, int64_t ld) {
+  return rows_of(p, ld == 0 ? 1 : (rows + per - 1) / per, cols, ld, 4);
+}
+
+ff_status check_gemm_i8(const ff_gemm_i8_desc* d, bool gate, bool resid) {
+  CHECK(d, FF_E_NULL, "gemm descriptor is NULL");
+  CHECK(d->a_dtype == FF_I8 || dtype_ok(d->a_dtype), FF_E_DTYPE, "unknown a_dtype %d", d->a_dtype);
+  CHECK(dtype_ok(d->out_dtype), FF_E_DTYPE, "unknown dtype %d", d->out_dtype);
+  CHECK(d->gelu == 0 || d->gelu == 1, FF_E_RANGE, "gelu must be 0 or 1");
+  CHECK(d->M >= 0 && d->M <= kMaxRows, FF_E_SHAPE, "M=%d outside [0, 2^23]", d->M);
+  CHECK(d->N >= 8 && d->N % 8 == 0 && d->N <= 1 << 20 && (int64_t)d->M * d->N <= (int64_t)1 << 34, FF_E_SHAPE,
+        "N=%d must be a multiple of 8 in [8, 2^20] with M * N <= 2^34", d->N);
+  CHECK(d->K >= 16 && d->K % 16 == 0 && d->K <= kI8MaxK, FF_E_SHAPE, "K=%d must be a multiple of 16 in [16, %d]", d->K, kI8MaxK);
+  CHECK(pitch_ok(d->a_row, d->K, d->a_dtype == FF_I8 ? 16 : 8) && pitch_ok(d->w_row, d->K, 16), FF_E_SHAPE,
+        "a_row and w_row must be >= K and multiples of 16 (a_row of 8 where A is not in 8 bits)");
+  CHECK(pitch_ok(d->out_row, d->N, 8) && (!resid || pitch_ok(d->resid_row, d->N, 8)), FF_E_SHAPE,
+        "out_row and resid_row must be multiples of 8 and >= N");
+  CHECK(!gate || d->gate_rows >= 1, FF_E_RANGE, "gate_rows=%d must be >= 1", d->gate_rows);
+  CHECK(!gate || vectors_ok(d->gate_ld, d->N), FF_E_SHAPE, "gate_ld must be 0, or a multiple of 8 and >= N");
+  const int64_t lim = 0x7fffff00ll;   // byte offsets inside a tile's buffers are 32 bits wide
+  CHECK((d->a_dtype != FF_I8 || (wide)256 * d->a_row < lim) && (wide)256 * d->w_row < lim, FF_E_SHAPE,
+        "256 operand rows must lie within 2^31 bytes");
+  return FF_OK;
+}
+
+bool norm_kind_ok(int k) { return k >= FF_NORM_NONE && k <= FF_NORM_LAYER; }
+
+ff_status check_branch(const ff_branch_norm_desc* d, bool branch, bool gate, bool mod, bool sum, bool y, bool q) {
+  CHECK(d, FF_E_NULL, "norm descriptor is NULL");
+  CHECK(dtype_ok(d->dtype), FF_E_DTYPE, "unknown dtype %d", d->dtype);
+  CHECK(norm_kind_ok(d->post) && norm_kind_ok(d->pre), FF_E_RANGE, "post=%d or pre=%d is no norm", d->post, d->pre);
+  CHECK(d->gate_tanh == 0 || d->gate_tanh == 1, FF_E_RANGE, "gate_tanh must be 0 or 1");
+  CHECK(d->eps > 0.f && isfinite(d->eps), FF_E_RANGE, "eps must be > 0");
+  CHECK(isfinite(d->resid_scale), FF_E_RANGE, "resid_scale must be finite");
+  CHECK(!(gate || mod) || d->mod_rows >= 1, FF_E_RANGE, "mod_rows=%d must be >= 1", d->mod_rows);
+  CHECK(d->rows >= 0 && d->rows <= kMaxRows, FF_E_SHAPE, "rows=%d outside [0, 2^23]", d->rows);
+  CHECK(d->C >= 8 && d->C % 8 == 0 && d->C <= kNormMaxC, FF_E_SHAPE, "C=%d must be a multiple of 8 in [8, %d]", d->C, kNormMaxC);
+  CHECK(pitch_ok(d->x_row, d->C, 8), FF_E_SHAPE, "x_row must be a multiple of 8 and >= C");
+  CHECK(!branch || pitch_ok(d->branch_row, d->C, 8), FF_E_SHAPE, "branch_row must be a multiple of 8 and >= C");
+  CHECK(!sum || pitch_ok(d->sum_row, d->C, 8), FF_E_SHAPE, "sum_row must be a multiple of 8 and >= C");
+  CHECK(!y || pitch_ok(d->y_row, d->C, 8), FF_E_SHAPE, "y_row must be a multiple of 8 and >= C");
+  CHECK(!q || pitch_ok(d->q_row, d->C, 8), FF_E_SHAPE, "q_row must be a multiple of 8 and >= C");
+  CHECK((!gate || vectors_ok(d->gate_ld, d->C)) && (!mod || vectors_ok(d->mod_ld, d->C)), FF_E_SHAPE,
+        "gate_ld and mod_ld must be 0, or multiples of 8 and >= C");
   return FF_OK;
 }
 
@@ -227,6 +285,88 @@ ff_status ff_gemm_q8(const ff_gemm_q8_desc* d, const void* a, const float* a_s, 
   const GemmQ8Args g{(const uint8_t*)a, d->a_row, a_s, d->as_ld, (const uint8_t*)w, d->w_row, w_s, d->ws_ld, bias, resid,
                      d->resid_row, out, d->out_row, d->M, d->N, d->K, d->gelu, need ? (float*)ws : nullptr};
   HIP_TRY(gemm_q8(d->out_dtype, g, reinterpret_cast<hipStream_t>(stream)), "8-bit gemm");
+  return ok();
+}
+
+ff_status ff_quant_i8(const ff_quant_i8_desc* d, const void* x, void* q, float* s, ff_stream_t stream) {
+  const ff_status e = check_quant_i8(d);
+  if (e) return e;
+  if (d->rows == 0) return ok();
+  CHECK(x && q && s, FF_E_NULL, "x, q or s is NULL");
+  CHECK(aligned16(x) && aligned16(q) && aligned16(s), FF_E_SHAPE, "pointers must be 16-byte aligned");
+  const Extent ex = rows_of(x, d->rows, d->C, d->x_row, (int)dsize(d->dtype)), eq = rows_of(q, d->rows, d->C, d->q_row, 1),
+               es = rows_of(s, 1, d->rows, d->rows, 4);
+  CHECK(!ex.meets(eq) && !ex.meets(es) && !eq.meets(es), FF_E_SHAPE, "x, q and s must not overlap");
+  HIP_TRY(quant_i8(d->dtype, QuantI8Args{x, d->x_row, (uint8_t*)q, d->q_row, s, d->rows, d->C}, reinterpret_cast<hipStream_t>(stream)),
+          "8-bit integer quantisation");
+  return ok();
+}
+
+size_t ff_gemm_i8_workspace_bytes(const ff_gemm_i8_desc* d) {
+  return check_gemm_i8(d, false, false) ? 0 : gemm_i8_workspace(d->a_dtype, d->out_dtype, d->M, d->N, d->K);
+}
+
+ff_status ff_gemm_i8(const ff_gemm_i8_desc* d, const void* a, const float* a_s, const void* w, const float* w_s, const void* bias,
+                     const float* gate, const void* resid, void* out, void* ws, size_t ws_bytes, ff_stream_t stream) {
+  const ff_status e = check_gemm_i8(d, gate != nullptr, resid != nullptr);
+  if (e) return e;
+  if (d->M == 0) return ok();
+  CHECK(a && w && w_s && out, FF_E_NULL, "a, w, w_s or out is NULL");
+  CHECK((d->a_dtype == FF_I8) == (a_s != nullptr), FF_E_NULL, "a_s and a_dtype disagree");
+  const size_t need = gemm_i8_workspace(d->a_dtype, d->out_dtype, d->M, d->N, d->K);
+  CHECK(!need || ws, FF_E_NULL, "ws is NULL");
+  CHECK(ws_bytes >= need, FF_E_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
+  const void* ps[] = {a, a_s, w, w_s, bias, gate, resid, out, need ? ws : nullptr};
+  for (const void* p : ps) CHECK(!p || aligned16(p), FF_E_SHAPE, "pointers must be 16-byte aligned");
+  const int es = (int)dsize(d->out_dtype);
+  const Extent in[7] = {rows_of(a, d->M, d->K, d->a_row, d->a_dtype == FF_I8 ? 1 : (int)dsize(d->a_dtype)), rows_of(a_s, 1, d->M, d->M, 4),
+                        rows_of(w, d->N, d->K, d->w_row, 1), rows_of(w_s, 1, d->N, d->N, 4), rows_of(bias, 1, d->N, d->N, es),
+                        gate ? vectors_of(gate, d->M, d->gate_rows, d->N, d->gate_ld) : Extent{nullptr, 0, 0, 0},
+                        rows_of(resid, d->M, d->N, d->resid_row, es)};
+  const Extent eo = rows_of(out, d->M, d->N, d->out_row, es), ew{(const char*)ws, (wide)need, 0, 0};
+  for (int i = 0; i < 7; ++i) {
+    CHECK(!ew.meets(in[i]), FF_E_SHAPE, "the workspace overlaps an input");
+    if (i == 6 && out == resid && d->out_row == d->resid_row) continue;   // each element is read by the lane that writes it
+    CHECK(!eo.meets(in[i]), FF_E_SHAPE, "out overlaps an input");
+  }
+  CHECK(!eo.meets(ew), FF_E_SHAPE, "out overlaps the workspace");
+  const GemmI8Args g{a, d->a_row, a_s, (const uint8_t*)w, d->w_row, w_s, bias, resid, d->resid_row, gate, d->gate_ld, d->gate_rows,
+                     out, d->out_row, d->M, d->N, d->K, d->gelu, need ? (int*)ws : nullptr};
+  HIP_TRY(gemm_i8(d->a_dtype, d->out_dtype, g, reinterpret_cast<hipStream_t>(stream)), "8-bit integer gemm");
+  return ok();
+}
+
+ff_status ff_branch_norm_i8(const ff_branch_norm_desc* d, const void* x, const void* branch, const void* post_gain, const float* gate,
+                            const void* pre_gain, const float* scale, const float* shift, void* sum, void* y, void* q, float* q_s,
+                            ff_stream_t stream) {
+  const ff_status e = check_branch(d, branch != nullptr, gate != nullptr, scale || shift, sum != nullptr, y != nullptr, q != nullptr);
+  if (e) return e;
+  if (d->rows == 0) return ok();
+  CHECK(x, FF_E_NULL, "x is NULL");
+  CHECK(sum || y || q, FF_E_NULL, "sum, y and q are all NULL");
+  CHECK((q == nullptr) == (q_s == nullptr), FF_E_NULL, "q and q_s go together");
+  CHECK(branch || (!post_gain && !gate), FF_E_NULL, "post_gain and gate need branch");
+  const void* ps[] = {x, branch, post_gain, gate, pre_gain, scale, shift, sum, y, q, q_s};
+  for (const void* p : ps) CHECK(!p || aligned16(p), FF_E_SHAPE, "pointers must be 16-byte aligned");
+  const int es = (int)dsize(d->dtype);
+  auto vec = [&](const float* p, int64_t ld) { return p ? vectors_of(p, d->rows, d->mod_rows, d->C, ld) : Extent{nullptr, 0, 0, 0}; };
+  const Extent in[7] = {rows_of(x, d->rows, d->C, d->x_row, es), rows_of(branch, d->rows, d->C, d->branch_row, es),
+                        rows_of(post_gain, 1, d->C, d->C, es), vec(gate, d->gate_ld), rows_of(pre_gain, 1, d->C, d->C, es),
+                        vec(scale, d->mod_ld), vec(shift, d->mod_ld)};
+  const Extent out[4] = {rows_of(sum, d->rows, d->C, d->sum_row, es), rows_of(y, d->rows, d->C, d->y_row, es),
+                         rows_of(q, d->rows, d->C, d->q_row, 1), rows_of(q_s, 1, d->rows, d->rows, 4)};
+  for (int o = 0; o < 4; ++o) {
+    for (int i = 0; i < 7; ++i) {
+      // the sum may take the place of the residual or the branch: a row's loads precede its stores
+      if (o == 0 && ((i == 0 && sum == x && d->sum_row == d->x_row) || (i == 1 && sum == branch && d->sum_row == d->branch_row))) continue;
+      CHECK(!out[o].meets(in[i]), FF_E_SHAPE, "an output overlaps an input");
+    }
+    for (int p = 0; p < o; ++p) CHECK(!out[o].meets(out[p]), FF_E_SHAPE, "two outputs overlap");
+  }
+  const BranchArgs a{x, d->x_row, branch, d->branch_row, post_gain, pre_gain, gate, d->gate_ld, scale, shift, d->mod_ld, sum, d->sum_row,
+                     y, d->y_row, (uint8_t*)q, d->q_row, q_s, d->rows, d->C, d->post, d->pre, d->gate_tanh,
+                     d->mod_rows < 1 ? d->rows : d->mod_rows, d->eps, d->resid_scale};
+  HIP_TRY(branch_norm(d->dtype, a, reinterpret_cast<hipStream_t>(stream)), "norm between branches");
   return ok();
 }
 

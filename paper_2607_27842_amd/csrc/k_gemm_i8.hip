@@ -7,15 +7,88 @@
 // 4 (l / 16) + 0..3.  Lane l of an operand takes row l % 16 and 16 bytes of the 64 k.
 #include "gemm_8bit.h"
 #include "i8_common.h"
+#include <math.h>
 
 namespace ff {
 
 namespace {
 
 typedef int i32x4_t __attribute__((ext_vector_type(4)));
+typedef int i32x16_t __attribute__((ext_vector_type(16)));
 
 __device__ __forceinline__ i32x4_t mfma_i8(u32x4_t a, u32x4_t b, i32x4_t c) {
   return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4_t, a), __builtin_bit_cast(i32x4_t, b), c, 0, 0, 0);
+}
+
+__device__ __forceinline__ i32x16_t mfma_i8(u32x4_t a, u32x4_t b, i32x16_t c) {
+  return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4_t, a), __builtin_bit_cast(i32x4_t, b), c, 0, 0, 0);
+}
+
+// ---------------------------------------------------------------- epilogue
+// Bias, activation and gate of 8 columns c.. of row r, on the sums times both scales
+template <int DT>
+__device__ __forceinline__ void act_gate(const GemmI8Args& a, int r, int c, const float* bias, float (&v)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] += bias[e];
+  if (a.gelu) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = gelu_tanh_f(v[e]);
+  }
+  if (a.gate) {
+    float g[8];
+    load8<DT_F32>(a.gate, (size_t)((uint32_t)r / (uint32_t)a.gate_rows) * a.gate_ld + c, g);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= g[e];
+  }
+}
+
+// Rows r0 .. r0 + RB NB - 1, columns c0 .. c0 + WN - 1 of a wavefront: put(i) lays RB rows of sums at a time into
+// the wave's own LDS region, a row every WN + 4 words, and they come back as 8-column pieces, so that
+// every load and store of bias, gate, residual and output is 16 bytes wide and covers whole row segments (in
+// the MFMA layout each store would put 8 bytes into each of 16 or 32 rows).  N % 8 == 0: a piece is in range as
+// a whole.  The caller has retired all waves' reads of what the region overlays.
+template <int DT, int WN, int RB, int NB, class F>
+__device__ __forceinline__ void epilogue(const GemmI8Args& a, int r0, int c0, int* lds, F&& put) {
+  constexpr int LDW = WN + 4, CPR = WN / 8, RPP = 64 / CPR, NPASS = RB / RPP;
+  static_assert(64 % CPR == 0 && NPASS >= 1, "whole rows a pass");
+  const int lane = threadIdx.x & 63;
+  const int pc = lane % CPR * 8, pr = lane / CPR, c = c0 + pc;
+  const int cl = c < a.N ? c : 0;   // loads past the matrix read its first column or last row
+  float bias[8], sw[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) bias[e] = 0.f;
+  if (a.bias) load8<DT>(a.bias, cl, bias);
+  load8<DT_F32>(a.w_s, cl, sw);
+  // the rows' scales and the residual's pieces are requested a block ahead
+  typedef typename Raw8<DT>::type raw_t;
+  raw_t res[2][NPASS];
+  float sa[2][NPASS];
+  auto request = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+    for (int p = 0; p < NPASS; ++p) {
+      const int r = min(r0 + i * RB + p * RPP + pr, a.M - 1);
+      sa[i & 1][p] = a.a_s[r];
+      if (a.resid) res[i & 1][p] = Raw8<DT>::load(a.resid, (size_t)r * a.resid_row + cl);
+    }
+  };
+  request(0);
+#pragma unroll
+  for (int i = 0; i < NB; ++i) {
+    put(i);
+    if (i + 1 < NB) request(i + 1);
+#pragma unroll
+    for (int p = 0; p < NPASS; ++p) {
+      const int r = r0 + i * RB + p * RPP + pr;
+      const i32x4_t x0 = *reinterpret_cast<const i32x4_t*>(lds + (p * RPP + pr) * LDW + pc);
+      const i32x4_t x1 = *reinterpret_cast<const i32x4_t*>(lds + (p * RPP + pr) * LDW + pc + 4);
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = (float)(e < 4 ? x0[e & 3] : x1[e & 3]) * sa[i & 1][p] * sw[e];
+      act_gate<DT>(a, min(r, a.M - 1), cl, bias, v);
+      if (a.resid) Raw8<DT>::add(res[i & 1][p], v);
+      if (r < a.M && c < a.N) store8<DT>(a.out, (size_t)r * a.out_row + c, v);
+    }
+  }
 }
 
 // Few rows: 16 x 16 tile, operands straight from memory, the NW waves of a workgroup on interleaved blocks of 128 k;
@@ -76,6 +149,406 @@ __global__ __launch_bounds__(NW * 64) void k_gemm_i8_dir(GemmI8Args a) {
   else *reinterpret_cast<f32x4_t*>(reinterpret_cast<float*>(a.out) + o) = v;
 }
 
+// ---------------------------------------------------------------- large grids: two wave groups in turn
+// 256 x 256 tile, a stage of 128 k, 8 waves in two groups of four, one wave of each group per SIMD; a stage has
+// four phases, one per 32 rows of a wave's 128 x 64 block.  A phase is a memory part (fragment reads,
+// DMA) and 8 MFMAs of 32 x 32 x 32, with a barrier after each; the second group runs half a phase behind, so that
+// on every SIMD one wave's MFMAs (256 cycles) cover the other's reads and DMA.
+//
+// Operands: 64-row pieces of 8 KB, each filled by one DMA instruction per wave, in two buffers per operand.  Phase
+// p of stage k issues, in this order:
+//   0: A3 of stage k+1   1: A0, B0, B1 of k+2   2: A1, B2 of k+2   3: A2, B3 of k+2
+// and reads: phase 0 all B and A0 of stage k, phases 1-3 A1-A3.  So a piece's slot is refilled no earlier than
+// one phase after its last read.
+// K % 128 != 0: the last stage's chunks past K are out of the resource's range and load zeros.
+constexpr int kPPIssue[4][3] = {{3, -1, -1}, {0, 4, 5}, {1, 6, -1}, {2, 7, -1}};   // A0-A3, B0-B3
+// How many of a wave's DMAs may be outstanding at the end of phase p of a stage with `left` stages
+// after it (2: two or more), so that what phase p + 1 reads has landed.
+constexpr int pp_vm(int p, int left) {
+  int n = 0, need = -1;
+  for (int j = -2; j <= 0; ++j)
+    for (int q = 0; q < (j == 0 ? p + 1 : 4); ++q)
+      for (int i = 0; i < 3; ++i) {
+        const int pc = kPPIssue[q][i], st = pc == 3 ? j + 1 : j + 2;
+        if (pc < 0 || st > left) continue;
+        ++n;
+        const bool next = (p == 0 && pc == 1 && st == 0) || (p == 1 && pc == 2 && st == 0) ||
+                          (p == 2 && pc == 3 && st == 0) || (p == 3 && (pc == 0 || pc >= 4) && st == 1);
+        if (next) need = n;
+      }
+  return need < 0 ? 63 : n - need;
+}
+
+template <int DT>
+__global__ __launch_bounds__(512) void k_gemm_i8_pp(GemmI8Args a) {
+#ifdef __HIP_DEVICE_COMPILE__   // the host pass needs the launch stub only
+  constexpr int BM = 256, BN = 256, TN = 4, WN = 16 * TN, RB = kQBlock;   // RB: bytes of an LDS row
+  constexpr int PC = 64 * RB, BUFA = 4 * PC, BUFB = TN * PC, OFFB = 2 * BUFA;
+  constexpr int kMain = OFFB + 2 * BUFB, kEpi = 8 * 32 * (WN + 4) * 4;
+  __shared__ __attribute__((aligned(1024))) char lds[kMain > kEpi ? kMain : kEpi];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int tm, tn;
+  tile_at(blockIdx.x, gridDim.x, (a.M + BM - 1) / BM, (a.N + BN - 1) / BN, tm, tn);
+  const int m0 = tm * BM, n0 = tn * BN;
+  const int mw = wave >> 2, nw = wave & 3;
+  const int nk = (a.K + kQBlock - 1) / kQBlock;   // >= 3 (host check)
+  // Piece Aq holds rows 32 q .. 32 q + 31 of both wave rows, piece Bu columns 16 u .. 16 u + 15 of all
+  // four wave columns.  Rows past the matrix read the tile's first row (never stored).
+  auto rsrc = [](const void* p) __attribute__((always_inline)) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, 0x7fffff00u, 0x00020000);
+  };
+  __amdgpu_buffer_rsrc_t ra = rsrc(static_cast<const uint8_t*>(a.a) + (size_t)m0 * a.a_row), rw = rsrc(a.w + (size_t)n0 * a.w_row);
+  const int R = wave * 8 + (lane >> 3);
+  const uint32_t ch = ((lane & 7) ^ ((R >> 1) & 7)) * 16;
+  uint32_t voa[4], vob[TN];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int r = (R >> 5) * 128 + q * 32 + (R & 31);
+    voa[q] = (m0 + r < a.M ? (uint32_t)r * (uint32_t)a.a_row : 0u) + ch;
+  }
+#pragma unroll
+  for (int u = 0; u < TN; ++u) {
+    const int r = (R >> 4) * WN + u * 16 + (R & 15);
+    vob[u] = (n0 + r < a.N ? (uint32_t)r * (uint32_t)a.w_row : 0u) + ch;
+  }
+  const bool cut = (int)ch >= a.K - (nk - 1) * kQBlock;   // this lane's chunk of the last stage lies past K
+#define FF_DMA(rs, vo, dst, kb) __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, FF_AS3(lds + (dst) + wave * 1024), 16, vo, kb, 0, 0)
+  i32x16_t acc[4][2];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
+  // lane l of a fragment: row l % 32, 16-byte chunk 2 s + l / 32 of its 128 (s: the MFMA's 32 k); columns 16 .. 31 of a B
+  // fragment stand in the next piece
+  const uint32_t lds0 = (uint32_t)(uintptr_t)((__attribute__((address_space(3))) const void*)lds);
+  const int fr = lane & 31, fh = lane >> 5;
+  uint32_t rda[4], rdb[4];   // fragment addresses, current buffers
+#pragma unroll
+  for (int s = 0; s < 4; ++s) {
+    const uint32_t c = ((2 * s + fh) ^ ((fr >> 1) & 7)) * 16;
+    rda[s] = lds0 + (mw * 32 + fr) * RB + c;
+    rdb[s] = lds0 + OFFB + (fr >> 4) * PC + (nw * 16 + (fr & 15)) * RB + c;
+  }
+  u32x4_t fa[4], fb[2][4];
+  int kb = 0, ca = 0, cb = 0;   // this stage's byte offset along K, and its buffers
+#define FF_RDA(off)                                                                               \
+  do {                                                                                            \
+    _Pragma("unroll") for (int s = 0; s < 4; ++s) fa[s] = __builtin_bit_cast(u32x4_t, lds_rd128_at<(off)>(rda[s])); \
+  } while (0)
+#define FF_MEM_END() asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory")
+#define FF_MMA(q)                                                                                   \
+  do {                                                                                              \
+    _Pragma("unroll") for (int s = 0; s < 4; ++s) FF_TIE(fa[s]);                                    \
+    __builtin_amdgcn_sched_barrier(0);                                                              \
+    __builtin_amdgcn_s_setprio(1);                                                                  \
+    _Pragma("unroll") for (int s = 0; s < 4; ++s)                                                   \
+      _Pragma("unroll") for (int u = 0; u < 2; ++u) acc[q][u] = mfma_i8(fb[u][s], fa[s], acc[q][u]); \
+    __builtin_amdgcn_s_setprio(0);                                                                  \
+    __builtin_amdgcn_sched_barrier(0);                                                              \
+    asm volatile("s_barrier" ::: "memory");                                                         \
+  } while (0)
+  auto stage = [&](auto LEFTc) __attribute__((always_inline)) {
+    constexpr int LEFT = decltype(LEFTc)::value;
+    constexpr bool k1 = LEFT >= 1, k2 = LEFT >= 2;
+    const int oa = BUFA - ca, ob = BUFB - cb;
+    // phase 0
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int s = 0; s < 4; ++s) fb[u][s] = __builtin_bit_cast(u32x4_t, lds_rd128_off(rdb[s], u * 2 * PC));
+    FF_RDA(0);
+    if (k1) FF_DMA(ra, voa[3], 3 * PC + oa, kb + RB);
+    wait_vm<pp_vm(0, LEFT)>();
+    FF_MEM_END();
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int s = 0; s < 4; ++s) FF_TIE(fb[u][s]);
+    FF_MMA(0);
+    // phase 1
+    FF_RDA(1 * PC);
+    if (k2) {
+      FF_DMA(ra, voa[0], ca, kb + 2 * RB);
+      FF_DMA(rw, vob[0], OFFB + cb, kb + 2 * RB);
+      FF_DMA(rw, vob[1], OFFB + PC + cb, kb + 2 * RB);
+    }
+    wait_vm<pp_vm(1, LEFT)>();
+    FF_MEM_END();
+    FF_MMA(1);
+    // phase 2
+    FF_RDA(2 * PC);
+    if (k2) {
+      FF_DMA(ra, voa[1], PC + ca, kb + 2 * RB);
+      FF_DMA(rw, vob[2], OFFB + 2 * PC + cb, kb + 2 * RB);
+    }
+    wait_vm<pp_vm(2, LEFT)>();
+    FF_MEM_END();
+    FF_MMA(2);
+    // phase 3
+    FF_RDA(3 * PC);
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      rda[s] += oa - ca;
+      rdb[s] += ob - cb;
+    }
+    if (k2) {
+      FF_DMA(ra, voa[2], 2 * PC + ca, kb + 2 * RB);
+      FF_DMA(rw, vob[3], OFFB + 3 * PC + cb, kb + 2 * RB);
+    }
+    wait_vm<pp_vm(3, LEFT)>();
+    FF_MEM_END();
+    FF_MMA(3);
+    kb += RB;
+    ca = oa;
+    cb = ob;
+  };
+  // prologue: what the stages -2 and -1 would have issued, in that order
+#pragma unroll
+  for (int j = -2; j < 0; ++j)
+#pragma unroll
+    for (int q = 0; q < 12; ++q) {
+      const int pc = kPPIssue[q / 3][q % 3], s = pc == 3 ? j + 1 : j + 2;
+      if (pc < 0 || s < 0) continue;
+      if (pc < 4) FF_DMA(ra, voa[pc & 3], s * BUFA + pc * PC, s * RB);
+      else FF_DMA(rw, vob[pc & 3], OFFB + s * BUFB + (pc - 4) * PC, s * RB);
+    }
+  wait_vm<3 + TN>();   // stage 0 has landed, and stage 1 but for A3 is on its way
+  asm volatile("s_barrier" ::: "memory");
+  if (wave >= 4) asm volatile("s_barrier" ::: "memory");   // the second group runs half a phase behind
+  int left = nk - 2;   // >= 1
+  do {
+    if (left == 1) {   // the pieces issued from here on are the last stage's, but for A3 of the last but one
+#pragma unroll
+      for (int q = 0; q < 3; ++q) voa[q] = cut ? 0x80000000u : voa[q];
+#pragma unroll
+      for (int u = 0; u < TN; ++u) vob[u] = cut ? 0x80000000u : vob[u];
+    }
+    stage(Int<2>{});
+  } while (--left);
+  voa[3] = cut ? 0x80000000u : voa[3];
+  stage(Int<1>{});
+  stage(Int<0>{});
+  if (wave < 4) asm volatile("s_barrier" ::: "memory");
+#undef FF_MEM_END
+#undef FF_DMA
+#undef FF_RDA
+#undef FF_MMA
+  // every wave's LDS reads and DMA ended before the last barrier
+  int* const own = reinterpret_cast<int*>(lds) + wave * 32 * (WN + 4);
+  epilogue<DT, WN, 32, 4>(a, m0 + mw * 128, n0 + nw * WN, own, [&](int i) __attribute__((always_inline)) {
+    // lane l: row l % 32, columns 8 j + 4 (l / 32) + 0..3
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<i32x4_t*>(own + fr * (WN + 4) + 32 * u + 8 * j + 4 * fh) =
+            i32x4_t{acc[i][u][4 * j], acc[i][u][4 * j + 1], acc[i][u][4 * j + 2], acc[i][u][4 * j + 3]};
+  });
+#endif
+}
+
+// ---------------------------------------------------------------- smaller grids
+// BM x BN tile, 8 waves in two groups of four; a group takes every second block of K for the whole tile
+// (2 x 2 waves), so that a fragment read feeds up to four MFMAs, and has its own ring of NS blocks.
+// Per block a wave has a memory slot (its fragments) and a matrix slot (the MFMAs, and behind each a DMA of the block
+// NS ahead into the ring slot just read), each ended by a barrier; the second group runs one slot
+// behind, one wave of each group per SIMD.  The two groups' sums meet in LDS: each finishes half of the rows.
+template <int DT, int BM, int BN, int NS>
+__global__ __launch_bounds__(512) void k_gemm_i8_two(GemmI8Args a, int splits) {
+#ifdef __HIP_DEVICE_COMPILE__   // the host pass needs the launch stub only
+  constexpr int TM = BM / 32, TN = BN / 32, WN = BN / 2, RB = kQBlock;
+  constexpr int STB = (BM + BN) * RB;   // bytes of a block
+  constexpr int NA = BM / 32, NW = BN / 32, PER = NA + NW;   // DMA instructions of a wave and block
+  constexpr int kMain = 2 * NS * STB;
+  constexpr int HT = TM / 2, kXch = 8 * HT * TN * 1024, RE = HT > 1 ? 32 : 16, kEpi = kXch + 8 * RE * (WN + 4) * 4;
+  static_assert(TM % 2 == 0 && PER <= 2 * TM * TN, "halves of the rows; a DMA behind an MFMA");
+  __shared__ __attribute__((aligned(1024))) char lds[kMain > kEpi ? kMain : kEpi];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int grp = wave >> 2, w = wave & 3, wr = w >> 1, wc = w & 1;
+  int tm, tn;
+  const int tiles = gridDim.x / splits, split = (int)blockIdx.x / tiles;
+  tile_at((int)blockIdx.x - split * tiles, tiles, (a.M + BM - 1) / BM, (a.N + BN - 1) / BN, tm, tn);
+  const int m0 = tm * BM, n0 = tn * BN;
+  // this workgroup's blocks of K: [kb0, kb0 + nb)
+  const int nk = (a.K + kQBlock - 1) / kQBlock, kb0 = (int)((long)nk * split / splits), nb = (int)((long)nk * (split + 1) / splits) - kb0;
+  const int mine = (nb - grp + 1) / 2, turns = (nb + 1) / 2;
+  auto rsrc = [](const void* p) __attribute__((always_inline)) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, 0x7fffff00u, 0x00020000);
+  };
+  __amdgpu_buffer_rsrc_t ra = rsrc(static_cast<const uint8_t*>(a.a) + (size_t)m0 * a.a_row), rw = rsrc(a.w + (size_t)n0 * a.w_row);
+  // rows past the matrix read the tile's first row (never stored); chunks of the last block past K are
+  // out of the resource's range and load zeros
+  uint32_t voa[NA], vow[NW];
+  unsigned cut = 0;
+#pragma unroll
+  for (int j = 0; j < NA + NW; ++j) {
+    const int R = (w * (j < NA ? NA : NW) + (j < NA ? j : j - NA)) * 8 + (lane >> 3);
+    const uint32_t ch = ((lane & 7) ^ ((R >> 1) & 7)) * 16;
+    if (j < NA) voa[j < NA ? j : 0] = (m0 + R < a.M ? (uint32_t)R * (uint32_t)a.a_row : 0u) + ch;
+    else vow[j < NA ? 0 : j - NA] = (n0 + R < a.N ? (uint32_t)R * (uint32_t)a.w_row : 0u) + ch;
+    if ((int)ch >= a.K - (nk - 1) * kQBlock) cut |= 1u << j;
+  }
+  char* const ring = lds + grp * NS * STB;
+  auto issue1 = [&](int i, int slot, int j) __attribute__((always_inline)) {   // DMA j of the group's block i
+    const int kt = kb0 + 2 * i + grp, kb = kt * RB;
+    const unsigned c = kt == nk - 1 ? cut : 0u;
+    char* const dst = ring + slot * STB;
+    if (j < NA)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, FF_AS3(dst + (w * NA + j) * 1024), 16, voa[j < NA ? j : 0] | (c >> j & 1u) << 31, kb, 0, 0);
+    else
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, FF_AS3(dst + BM * RB + (w * NW + j - NA) * 1024), 16,
+                                               vow[j < NA ? 0 : j - NA] | (c >> j & 1u) << 31, kb, 0, 0);
+  };
+  i32x4_t acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) acc[i][j] = i32x4_t{0, 0, 0, 0};
+  const int fr = lane & 15, fh = lane >> 4;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)((__attribute__((address_space(3))) const void*)lds);
+  uint32_t rda[2], rdw[2];
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    const uint32_t c = ((4 * s + fh) ^ (fr >> 1)) * 16, o = lds0 + grp * NS * STB;
+    rda[s] = o + (wr * (BM / 2) + fr) * RB + c;
+    rdw[s] = o + (BM + wc * WN + fr) * RB + c;
+  }
+  u32x4_t fa[2 * TM], fw[2 * TN];
+#pragma unroll
+  for (int i = 0; i < NS; ++i)
+    if (i < mine) {
+#pragma unroll
+      for (int j = 0; j < PER; ++j) issue1(i, i, j);
+    }
+  wait_vm<0>();
+  asm volatile("s_barrier" ::: "memory");
+  if (grp) asm volatile("s_barrier" ::: "memory");   // the second group runs one slot behind
+  int slot = 0;
+  auto turn = [&](int i, auto Mc) __attribute__((always_inline)) {
+    constexpr bool more = decltype(Mc)::value != 0;   // a block NS ahead is left
+    // memory slot
+    const uint32_t so = slot * STB;
+#pragma unroll
+    for (int t = 0; t < TN; ++t)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) fw[2 * t + s] = __builtin_bit_cast(u32x4_t, lds_rd128_off(rdw[s] + so, t * 16 * RB));
+#pragma unroll
+    for (int t = 0; t < TM; ++t)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) fa[2 * t + s] = __builtin_bit_cast(u32x4_t, lds_rd128_off(rda[s] + so, t * 16 * RB));
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int t = 0; t < 2 * TN; ++t) FF_TIE(fw[t]);
+#pragma unroll
+    for (int t = 0; t < 2 * TM; ++t) FF_TIE(fa[t]);
+    asm volatile("s_barrier" ::: "memory");
+    // matrix slot
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int t = 0; t < TM; ++t) {
+          acc[t][j] = mfma_i8(fw[2 * j + s], fa[2 * t + s], acc[t][j]);
+          const int at = (s * TN + j) * TM + t;
+          if (more && at < PER) {
+            __builtin_amdgcn_sched_barrier(0);
+            issue1(i + NS, slot, at);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+    __builtin_amdgcn_s_setprio(0);
+    __builtin_amdgcn_sched_barrier(0);
+    // the next block has landed; the ones after it may be on their way
+    wait_vm<more ? (NS - 1) * PER : 0>();
+    slot = slot == NS - 1 ? 0 : slot + 1;
+    asm volatile("s_barrier" ::: "memory");
+  };
+  int i = 0;
+  for (; i < mine - NS; ++i) turn(i, Int<1>{});
+  for (; i < mine; ++i) turn(i, Int<0>{});
+  if (mine < turns) {   // the second group, one block short
+    asm volatile("s_barrier" ::: "memory");
+    asm volatile("s_barrier" ::: "memory");
+  }
+  if (!grp) asm volatile("s_barrier" ::: "memory");
+  // every wave's LDS reads and DMA ended before the last barrier; each group finishes half of the rows
+  i32x4_t* const xch = reinterpret_cast<i32x4_t*>(lds) + lane;
+  i32x4_t fin[HT][TN];
+  auto half = [&](auto Gc) __attribute__((always_inline)) {
+    constexpr int G = decltype(Gc)::value;
+#pragma unroll
+    for (int t = 0; t < HT; ++t)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        xch[((wave * HT + t) * TN + j) * 64] = acc[(1 - G) * HT + t][j];
+        fin[t][j] = acc[G * HT + t][j];
+      }
+  };
+  if (grp) half(Int<1>{});
+  else half(Int<0>{});
+  __syncthreads();
+#pragma unroll
+  for (int t = 0; t < HT; ++t)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) fin[t][j] += xch[(((wave ^ 4) * HT + t) * TN + j) * 64];
+  const int r0 = m0 + wr * (BM / 2) + grp * HT * 16, c0 = n0 + wc * WN;
+  if (splits > 1) {   // bare sums for k_gemm_i8_join, each lane's four columns of its rows
+    int* const part = a.part + (size_t)split * a.M * a.N;
+#pragma unroll
+    for (int t = 0; t < HT; ++t)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        const int r = r0 + 16 * t + fr, c = c0 + 16 * j + 4 * fh;
+        if (r < a.M && c < a.N) *reinterpret_cast<i32x4_t*>(part + (size_t)r * a.N + c) = fin[t][j];
+      }
+    return;
+  }
+  int* const own = reinterpret_cast<int*>(lds + kXch) + wave * RE * (WN + 4);
+  epilogue<DT, WN, RE, HT * 16 / RE>(a, r0, c0, own, [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < RE / 16; ++t)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) *reinterpret_cast<i32x4_t*>(own + (16 * t + fr) * (WN + 4) + 16 * j + 4 * fh) = fin[i * (RE / 16) + t][j];
+  });
+#endif
+}
+
+// Joins the splits of K: 8 columns of a row a thread
+template <int DT>
+__global__ __launch_bounds__(256) void k_gemm_i8_join(GemmI8Args a, int splits) {
+  const int per = a.N / 8;
+  const size_t id = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (id >= (size_t)a.M * per) return;
+  const int r = (int)(id / per), c = (int)(id % per) * 8;
+  i32x4_t s[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+  for (int i = 0; i < splits; ++i) {
+    const i32x4_t* p = reinterpret_cast<const i32x4_t*>(a.part + (size_t)i * a.M * a.N + id * 8);
+    s[0] += p[0];
+    s[1] += p[1];
+  }
+  float v[8], x[8];
+  const float sa = a.a_s[r];
+  load8<DT_F32>(a.w_s, c, x);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = (float)s[e / 4][e % 4] * sa * x[e];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = 0.f;
+  if (a.bias) load8<DT>(a.bias, c, x);
+  act_gate<DT>(a, r, c, x, v);
+  if (a.resid) {
+    load8<DT>(a.resid, (size_t)r * a.resid_row + c, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += x[e];
+  }
+  store8<DT>(a.out, (size_t)r * a.out_row + c, v);
+}
+
+// ---------------------------------------------------------------- choice
 long tiles(long M, long N, long t) { return ((M + t - 1) / t) * ((N + t - 1) / t); }
 
 // rows that the call puts in 8 bits itself, and their scales behind them
@@ -83,18 +556,60 @@ size_t rows_bytes(int a_dtype, int M, int K) { return a_dtype == DT_I8 ? 0 : ((s
 
 }  // namespace
 
-I8Plan gemm_i8_plan(int, int, int, int, int) { return I8Plan{I8_DIR, 1}; }
+// The kernel of a shape by estimated time (us)
+I8Plan gemm_i8_plan(int out_dtype, int M, int N, int K) {
+  const int nk = (K + kQBlock - 1) / kQBlock;
+  // us per block of K: few tiles, what 256 tiles add, and a round of all CUs (512 tiles of 64 x 64)
+  const double c6[3] = {0.21, 0.08, 0.50}, c12[3] = {0.42, 0.30, 0.71};
+  I8Plan best{I8_TILE128, 1};
+  double least = 1e30;
+  auto take = [&](int k, int splits, double us) {
+    if (us < least) { least = us; best = I8Plan{k, splits}; }
+  };
+  if (M <= 256) {
+    const double t = (double)tiles(M, N, 16), chain = 0.4 * ((nk + 15) / 16);
+    take(I8_DIR, 1, 2.5 + (t * nk * 0.45e-3 > chain ? t * nk * 0.45e-3 : chain));
+  }
+  for (int s = 1; s <= 8; s *= 2) {
+    if (s > 1 && nk / s < 8) break;
+    const double t = (double)tiles(M, N, 64) * s, nb = (double)nk / s;
+    const double main = t <= 256 ? (c6[0] + c6[1] * t / 256) * nb : ceil(t / 512) * c6[2] * nb;
+    take(I8_TILE64, s, 3.5 + main + (s > 1 ? 1.8 + s * (0.35 + 2.3e-6 * M * N) : 0.0));
+  }
+  const double t128 = (double)tiles(M, N, 128), t256 = (double)tiles(M, N, 256);
+  take(I8_TILE128, 1, 3.5 + (t128 <= 256 ? c12[0] + c12[1] * t128 / 256 : ceil(t128 / 256) * c12[2]) * nk);
+  if (nk >= 3) take(I8_TILE256, 1, 4.0 + ceil(t256 / 256) * 1.75 * nk);
+  return best;
+}
+
+namespace {
+
+template <int DT>
+hipError_t launch_i8(const GemmI8Args& a, const I8Plan& p, hipStream_t s) {
+  switch (p.kernel) {
+    case I8_DIR: FF_LAUNCH((k_gemm_i8_dir<DT, 8>), (unsigned)tiles(a.M, a.N, 16), 512, 0, s, a); break;
+    case I8_TILE64: FF_LAUNCH((k_gemm_i8_two<DT, 64, 64, 2>), (unsigned)(tiles(a.M, a.N, 64) * p.splits), 512, 0, s, a, p.splits); break;
+    case I8_TILE128: FF_LAUNCH((k_gemm_i8_two<DT, 128, 128, 2>), (unsigned)tiles(a.M, a.N, 128), 512, 0, s, a, 1); break;
+    case I8_TILE256: FF_LAUNCH((k_gemm_i8_pp<DT>), (unsigned)tiles(a.M, a.N, 256), 512, 0, s, a); break;
+  }
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.splits == 1) return e;
+  const size_t wg = ((size_t)a.M * (a.N / 8) + 255) / 256;
+  FF_LAUNCH(k_gemm_i8_join<DT>, (unsigned)wg, 256, 0, s, a, p.splits);
+  return hipGetLastError();
+}
+
+}  // namespace
 
 size_t gemm_i8_workspace(int a_dtype, int out_dtype, int M, int N, int K) {
   if (M <= 0) return 0;
-  const int n = gemm_i8_plan(a_dtype, out_dtype, M, N, K).splits;
+  const int n = gemm_i8_plan(out_dtype, M, N, K).splits;
   return rows_bytes(a_dtype, M, K) + (n > 1 ? (size_t)n * M * N * 4 : 0);
 }
 
 hipError_t gemm_i8(int a_dtype, int out_dtype, const GemmI8Args& a0, hipStream_t s) {
   if (a0.M <= 0) return hipSuccess;
-  const long t = tiles(a0.M, a0.N, 16);
-  if (t > 0x7fffffffL) return hipErrorInvalidValue;
+  const I8Plan p = gemm_i8_plan(out_dtype, a0.M, a0.N, a0.K);
   GemmI8Args a = a0;
   if (a_dtype != DT_I8) {
     uint8_t* const q = reinterpret_cast<uint8_t*>(a0.part);
@@ -106,9 +621,7 @@ hipError_t gemm_i8(int a_dtype, int out_dtype, const GemmI8Args& a0, hipStream_t
     a.a_s = qs;
     a.part = reinterpret_cast<int*>(q + rows_bytes(a_dtype, a.M, a.K));
   }
-  if (out_dtype == DT_BF16) FF_LAUNCH((k_gemm_i8_dir<DT_BF16, 8>), (unsigned)t, 512, 0, s, a);
-  else FF_LAUNCH((k_gemm_i8_dir<DT_F32, 8>), (unsigned)t, 512, 0, s, a);
-  return hipGetLastError();
+  return out_dtype == DT_BF16 ? launch_i8<DT_BF16>(a, p, s) : launch_i8<DT_F32>(a, p, s);
 }
 
 }  // namespace ff

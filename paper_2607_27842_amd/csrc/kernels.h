@@ -223,7 +223,7 @@ enum { DT_I8 = 2 };
 // What a shape is run with: a kernel (its tile), and workgroups that share a tile's K
 enum { I8_DIR, I8_TILE64, I8_TILE128, I8_TILE256 };
 struct I8Plan { int kernel, splits; };
-I8Plan gemm_i8_plan(int a_dtype, int out_dtype, int M, int N, int K);
+I8Plan gemm_i8_plan(int out_dtype, int M, int N, int K);
 size_t gemm_i8_workspace(int a_dtype, int out_dtype, int M, int N, int K);
 hipError_t gemm_i8(int a_dtype, int out_dtype, const GemmI8Args& a, hipStream_t s);
 

@@ -6,39 +6,71 @@ namespace ff {
 
 namespace {
 
+// A row's values as they are stored: 8 columns a unit
+template <int DT> struct Piece;
+template <> struct Piece<DT_BF16> {
+  u32x4_t w;
+  __device__ __forceinline__ void load(const void* p, size_t i) { w = *reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(p) + i); }
+  __device__ __forceinline__ float at(int e) const { return __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16); }
+};
+template <> struct Piece<DT_F32> {
+  f32x4_t w[2];
+  __device__ __forceinline__ void load(const void* p, size_t i) {
+    const f32x4_t* q = reinterpret_cast<const f32x4_t*>(static_cast<const float*>(p) + i);
+    w[0] = q[0];
+    w[1] = q[1];
+  }
+  __device__ __forceinline__ float at(int e) const { return w[e / 4][e % 4]; }
+};
+
+// The largest of a row's wavefronts' values
+template <int W>
+__device__ __forceinline__ uint32_t top_row(uint32_t top, float* at, int wave) {
+  top = top64(top);
+  if (W == 1) return top;
+  if ((threadIdx.x & 63) == 0) at[wave] = __uint_as_float(top);
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < W; ++i) top = max(top, __float_as_uint(at[i]));
+  return top;
+}
+
 // ---------------------------------------------------------------- quantisation
 // W wavefronts hold a row, U units of 8 columns a lane, in registers between the row's largest value and
-// the rounding.
+// the rounding; a workgroup (or, W = 1, a wavefront) walks every step-th row, the next one's values requested ahead.
 template <int DT, int W, int U>
-__global__ __launch_bounds__(256) void k_quant_i8(QuantI8Args a) {
-  __shared__ uint32_t part[4];
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_quant_i8(QuantI8Args a, int step) {
+  __shared__ float part[2][W];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int row = blockIdx.x * (4 / W) + (W == 1 ? wave : 0), l = W == 1 ? lane : (int)threadIdx.x;
-  if (W == 1 && row >= a.rows) return;
-  float v[U][8];
+  const int l = W == 1 ? lane : (int)threadIdx.x;
+  int row = (W == 1 ? blockIdx.x * 4 + wave : blockIdx.x), turn = 0;
+  if (row >= a.rows) return;   // all of a row's wavefronts
+  Piece<DT> p[U];
+  auto request = [&](int r) __attribute__((always_inline)) {
 #pragma unroll
-  for (int i = 0; i < U; ++i) {
-    const int c = (l + 64 * W * i) * 8;
+    for (int i = 0; i < U; ++i)
+      if ((l + 64 * W * i) * 8 < a.C) p[i].load(a.x, (size_t)r * a.x_row + (l + 64 * W * i) * 8);
+  };
+  request(row);
+  for (;; row += step) {
+    float v[U][8];
+    uint32_t top = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
-    if (c < a.C) load8<DT>(a.x, (size_t)row * a.x_row + c, v[i]);
+    for (int i = 0; i < U; ++i) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] = (l + 64 * W * i) * 8 < a.C ? p[i].at(e) : 0.f;
+      top = top_bits<8>(v[i], top);
+    }
+    if (row + step < a.rows) request(row + step);
+    const I8Scale k(top_row<W>(top, part[turn++ & 1], wave));
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int c = (l + 64 * W * i) * 8;
+      if (c < a.C) *reinterpret_cast<u32x2_t*>(a.q + (size_t)row * a.q_row + c) = i8_pack8(v[i], k);
+    }
+    if (l == 0) a.s[row] = k.s;
+    if (row + step >= a.rows) break;
   }
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < U; ++i) top = top_bits<8>(v[i], top);
-  top = top64(top);
-  if (W > 1) {
-    if (lane == 0) part[wave] = top;
-    __syncthreads();
-    top = max(max(part[0], part[1]), max(part[2], part[3]));
-  }
-  const I8Scale k(top);
-#pragma unroll
-  for (int i = 0; i < U; ++i) {
-    const int c = (l + 64 * W * i) * 8;
-    if (c < a.C) *reinterpret_cast<u32x2_t*>(a.q + (size_t)row * a.q_row + c) = i8_pack8(v[i], k);
-  }
-  if (l == 0) a.s[row] = k.s;
 }
 
 // Rows too long for the registers are read twice.
@@ -63,21 +95,27 @@ __global__ __launch_bounds__(256) void k_quant_i8_long(QuantI8Args a) {
   if (threadIdx.x == 0) a.s[row] = k.s;
 }
 
+// As many walks as the card holds at once, each of W of about 6144 wavefronts (k_branch_norm, 14566 x 2048: 2048 walks
+// instead of 1536, 54.7 us for 50.4, as some start late; 3072 50.7, 8192 53.2).
+int walks_for(int rows, int W) { return rows < 6144 / W ? rows : 6144 / W; }
+
+template <int DT, int W, int U>
+void launch_quant_walks(const QuantI8Args& a, hipStream_t s) {
+  const int walks = walks_for(a.rows, W);
+  if (W == 1) FF_LAUNCH((k_quant_i8<DT, W, U>), (walks + 3) / 4, 256, 0, s, a, (walks + 3) / 4 * 4);
+  else FF_LAUNCH((k_quant_i8<DT, W, U>), walks, 64 * W, 0, s, a, walks);
+}
+
 template <int DT>
 void launch_quant(const QuantI8Args& a, hipStream_t s) {
   const int units = a.C / 8;
-  if (units <= 256 && a.rows >= 1024) {
-    const int wg = (a.rows + 3) / 4;
-    if (units <= 64) FF_LAUNCH((k_quant_i8<DT, 1, 1>), wg, 256, 0, s, a);
-    else if (units <= 128) FF_LAUNCH((k_quant_i8<DT, 1, 2>), wg, 256, 0, s, a);
-    else FF_LAUNCH((k_quant_i8<DT, 1, 4>), wg, 256, 0, s, a);
-  } else {
-    if (units <= 256) FF_LAUNCH((k_quant_i8<DT, 4, 1>), a.rows, 256, 0, s, a);
-    else if (units <= 512) FF_LAUNCH((k_quant_i8<DT, 4, 2>), a.rows, 256, 0, s, a);
-    else if (units <= 1024) FF_LAUNCH((k_quant_i8<DT, 4, 4>), a.rows, 256, 0, s, a);
-    else if (units <= 2048) FF_LAUNCH((k_quant_i8<DT, 4, 8>), a.rows, 256, 0, s, a);
-    else FF_LAUNCH(k_quant_i8_long<DT>, a.rows, 256, 0, s, a);
-  }
+  if (units <= 64) launch_quant_walks<DT, 1, 1>(a, s);
+  else if (units <= 128) launch_quant_walks<DT, 2, 1>(a, s);
+  else if (units <= 256) launch_quant_walks<DT, 4, 1>(a, s);
+  else if (units <= 512) launch_quant_walks<DT, 4, 2>(a, s);
+  else if (units <= 1024) launch_quant_walks<DT, 8, 2>(a, s);
+  else if (units <= 2048) launch_quant_walks<DT, 16, 2>(a, s);
+  else FF_LAUNCH(k_quant_i8_long<DT>, a.rows, 256, 0, s, a);
 }
 
 // ---------------------------------------------------------------- between branches
@@ -97,7 +135,11 @@ __device__ __forceinline__ float over_row(float v, float* at, int wave) {
   if (W == 1) return v;
   if ((threadIdx.x & 63) == 0) at[wave] = v;
   __syncthreads();
-  return (at[0] + at[1]) + (at[2] + at[3]);
+  if (W == 2) return at[0] + at[1];
+  float sum = (at[0] + at[1]) + (at[2] + at[3]);
+#pragma unroll
+  for (int i = 4; i < W; i += 4) sum += (at[i] + at[i + 1]) + (at[i + 2] + at[i + 3]);
+  return sum;
 }
 
 // v <- v normed.  Columns past the row hold zeros before and after.
@@ -121,104 +163,139 @@ __device__ __forceinline__ void norm_row(float (&v)[U][8], const BranchArgs& a, 
   for (int i = 0; i < U; ++i)
 #pragma unroll
     for (int e = 0; e < 8; ++e) ss = fmaf(v[i][e], v[i][e], ss);
-  const float inv = 1.0f / sqrtf(over_row<W>(ss, at + 4, wave) / (float)a.C + a.eps);
+  const float inv = 1.0f / sqrtf(over_row<W>(ss, at + W, wave) / (float)a.C + a.eps);
 #pragma unroll
   for (int i = 0; i < U; ++i)
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[i][e] *= inv;
 }
 
+// What a row's columns are multiplied by and moved by, the same for all rows of a sample
+template <int U>
+struct Vectors { float a[U][8], p[U][8], s[U][8]; };   // gate post_gain, pre_gain (1 + scale), shift
 template <int DT, int W, int U>
-__global__ __launch_bounds__(256) void k_branch_norm(BranchArgs a) {
-  __shared__ float part[20];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int row = blockIdx.x * (4 / W) + (W == 1 ? wave : 0), l = W == 1 ? lane : (int)threadIdx.x;
-  if (W == 1 && row >= a.rows) return;
-  const size_t smp = row / a.mod_rows;
-  float t[U][8], z[U][8], g[8], f[8];
+__device__ __forceinline__ void load_vectors(const BranchArgs& k, size_t smp, int l, Vectors<U>& v) {
 #pragma unroll
   for (int i = 0; i < U; ++i) {
     const int c = (l + 64 * W * i) * 8;
+    float g[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) t[i][e] = z[i][e] = 0.f;
-    if (c < a.C) {
-      load8<DT>(a.x, (size_t)row * a.x_row + c, t[i]);
-      if (a.branch) load8<DT>(a.branch, (size_t)row * a.branch_row + c, z[i]);
+    for (int e = 0; e < 8; ++e) { v.a[i][e] = v.p[i][e] = 1.f; v.s[i][e] = 0.f; }
+    if (c >= k.C) continue;
+    if (k.post_gain) load8<DT>(k.post_gain, c, v.a[i]);
+    if (k.gate) {
+      load8<DT_F32>(k.gate, smp * k.gate_ld + c, g);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v.a[i][e] *= k.gate_tanh ? tanh_f(g[e]) : g[e];
     }
+    if (k.pre_gain) load8<DT>(k.pre_gain, c, v.p[i]);
+    if (k.scale) {
+      load8<DT_F32>(k.scale, smp * k.mod_ld + c, g);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v.p[i][e] *= 1.0f + g[e];
+    }
+    if (k.shift) load8<DT_F32>(k.shift, smp * k.mod_ld + c, v.s[i]);
   }
-  if (a.branch) norm_row<W, U>(z, a, a.post, l, part, wave);
-#pragma unroll
-  for (int i = 0; i < U; ++i) {
-    const int c = (l + 64 * W * i) * 8;
-    if (c >= a.C) continue;
-    if (a.post_gain) {
-      load8<DT>(a.post_gain, c, g);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) z[i][e] *= g[e];
-    }
-    if (a.gate) {
-      load8<DT_F32>(a.gate, smp * a.gate_ld + c, g);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) z[i][e] *= a.gate_tanh ? tanh_f(g[e]) : g[e];
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) t[i][e] = St<DT>::rnd(fmaf(t[i][e], a.resid_scale, z[i][e]));
-    if (a.sum) store8<DT>(a.sum, (size_t)row * a.sum_row + c, t[i]);
-  }
-  if (!a.y && !a.q) return;
-  norm_row<W, U>(t, a, a.pre, l, part + 8, wave);
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < U; ++i) {
-    const int c = (l + 64 * W * i) * 8;
-    if (c >= a.C) continue;
-    if (a.pre_gain) {
-      load8<DT>(a.pre_gain, c, g);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) t[i][e] *= g[e];
-    }
-    if (a.scale) {
-      load8<DT_F32>(a.scale, smp * a.mod_ld + c, g);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) t[i][e] *= 1.0f + g[e];
-    }
-    if (a.shift) {
-      load8<DT_F32>(a.shift, smp * a.mod_ld + c, f);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) t[i][e] += f[e];
-    }
-    if (a.y) store8<DT>(a.y, (size_t)row * a.y_row + c, t[i]);
-    top = top_bits<8>(t[i], top);
-  }
-  if (!a.q) return;
-  top = top64(top);
-  if (W > 1) {
-    if (lane == 0) part[16 + wave] = __uint_as_float(top);
-    __syncthreads();
-    top = max(max(__float_as_uint(part[16]), __float_as_uint(part[17])), max(__float_as_uint(part[18]), __float_as_uint(part[19])));
-  }
-  const I8Scale k(top);
-#pragma unroll
-  for (int i = 0; i < U; ++i) {
-    const int c = (l + 64 * W * i) * 8;
-    if (c < a.C) *reinterpret_cast<u32x2_t*>(a.q + (size_t)row * a.q_row + c) = i8_pack8(t[i], k);
-  }
-  if (l == 0) a.q_s[row] = k.s;
 }
 
+// W wavefronts hold a row, U units of 8 columns a lane; a workgroup (or, W = 1, a wavefront) walks every step-th row.
+// The next row's values are requested before this row's sums meet, and the sample's vectors stay in registers
+// from row to row: read again for each row they are twice a bf16 row's own bytes, from L2.  Bound by memory: 14566 x 2048
+// bf16, both norms, gate, scale and shift, 50.4 us, 4.74 TB/s of the 5.0 that a large copy reaches; a row a
+// workgroup 60.3, walks of neighbouring rows 54.1.  One row 3.6 us, a launch.
+template <int DT, int W, int U>
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_branch_norm(BranchArgs a, int step) {
+  __shared__ float part[2][5 * W];   // a row's reductions have a place each, and rows in turn two sets
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int l = W == 1 ? lane : (int)threadIdx.x;
+  int row = (W == 1 ? blockIdx.x * 4 + wave : blockIdx.x);
+  int turn = 0;
+  if (row >= a.rows) return;   // all of a row's wavefronts
+  Piece<DT> px[U], pz[U];
+  auto request = [&](int r) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int c = (l + 64 * W * i) * 8;
+      if (c >= a.C) continue;
+      px[i].load(a.x, (size_t)r * a.x_row + c);
+      if (a.branch) pz[i].load(a.branch, (size_t)r * a.branch_row + c);
+    }
+  };
+  constexpr bool kAhead = W * U <= 16;   // the widest rows need the registers
+  if (kAhead) request(row);
+  Vectors<U> v;
+  int smp = row / a.mod_rows, next = min((smp + 1) * (int64_t)a.mod_rows, (int64_t)a.rows);   // the next sample's first row
+  load_vectors<DT, W, U>(a, smp, l, v);
+  for (;; row += step) {
+    float* const at = part[turn++ & 1];
+    float t[U][8], z[U][8];
+    if (!kAhead) request(row);
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const bool in = (l + 64 * W * i) * 8 < a.C;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        t[i][e] = in ? px[i].at(e) : 0.f;
+        z[i][e] = in && a.branch ? pz[i].at(e) : 0.f;
+      }
+    }
+    if (row >= next) {
+      smp = row / a.mod_rows;
+      next = min((smp + 1) * (int64_t)a.mod_rows, (int64_t)a.rows);
+      load_vectors<DT, W, U>(a, smp, l, v);
+    }
+    if (kAhead && row + step < a.rows) request(row + step);
+    if (a.branch) norm_row<W, U>(z, a, a.post, l, at, wave);
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int c = (l + 64 * W * i) * 8;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) t[i][e] = St<DT>::rnd(fmaf(t[i][e], a.resid_scale, z[i][e] * v.a[i][e]));
+      if (a.sum && c < a.C) store8<DT>(a.sum, (size_t)row * a.sum_row + c, t[i]);
+    }
+    if (a.y || a.q) {
+      norm_row<W, U>(t, a, a.pre, l, at + 2 * W, wave);
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int c = (l + 64 * W * i) * 8;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t[i][e] = fmaf(t[i][e], v.p[i][e], v.s[i][e]);
+        if (a.y && c < a.C) store8<DT>(a.y, (size_t)row * a.y_row + c, t[i]);
+        top = top_bits<8>(t[i], top);   // columns past C hold zeros
+      }
+      if (a.q) {
+        const I8Scale k(top_row<W>(top, at + 4 * W, wave));
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          const int c = (l + 64 * W * i) * 8;
+          if (c < a.C) *reinterpret_cast<u32x2_t*>(a.q + (size_t)row * a.q_row + c) = i8_pack8(t[i], k);
+        }
+        if (l == 0) a.q_s[row] = k.s;
+      }
+    }
+    if (row + step >= a.rows) break;
+  }
+}
+
+template <int DT, int W, int U>
+void launch_walks(const BranchArgs& a, hipStream_t s) {
+  const int walks = walks_for(a.rows, W);
+  if (W == 1) FF_LAUNCH((k_branch_norm<DT, W, U>), (walks + 3) / 4, 256, 0, s, a, (walks + 3) / 4 * 4);
+  else FF_LAUNCH((k_branch_norm<DT, W, U>), walks, 64 * W, 0, s, a, walks);
+}
+
+// One unit a lane where the row allows it (20000 x 1024: one wavefront with two 40.3 us, two with one 35.7; 4608 x 2048:
+// two wavefronts with two 18.9, four with one 16.2)
 template <int DT>
 void launch_branch(const BranchArgs& a, hipStream_t s) {
   const int units = a.C / 8;
-  if (units <= 128) {
-    const int wg = (a.rows + 3) / 4;
-    if (units <= 64) FF_LAUNCH((k_branch_norm<DT, 1, 1>), wg, 256, 0, s, a);
-    else FF_LAUNCH((k_branch_norm<DT, 1, 2>), wg, 256, 0, s, a);
-  } else {
-    if (units <= 256) FF_LAUNCH((k_branch_norm<DT, 4, 1>), a.rows, 256, 0, s, a);
-    else if (units <= 512) FF_LAUNCH((k_branch_norm<DT, 4, 2>), a.rows, 256, 0, s, a);
-    else if (units <= 1024) FF_LAUNCH((k_branch_norm<DT, 4, 4>), a.rows, 256, 0, s, a);
-    else FF_LAUNCH((k_branch_norm<DT, 4, 8>), a.rows, 256, 0, s, a);
-  }
+  if (units <= 64) launch_walks<DT, 1, 1>(a, s);
+  else if (units <= 128) launch_walks<DT, 2, 1>(a, s);
+  else if (units <= 256) launch_walks<DT, 4, 1>(a, s);
+  else if (units <= 512) launch_walks<DT, 8, 1>(a, s);
+  else if (units <= 1024) launch_walks<DT, 16, 1>(a, s);
+  else launch_walks<DT, 16, 2>(a, s);
 }
 
 }  // namespace

@@ -24,7 +24,8 @@ def rows_like(rows, C, g, dtype=F32):
 
 @TYPES
 @pytest.mark.parametrize("rows,C,pad", [(1, 8, 0), (1, 2048, 0), (3, 136, 24), (17, 1480, 8), (2, 4096, 0), (5, 8200, 16), (2, 16384, 0),
-                                        (2, 16400, 40), (1, 131056, 0), (1025, 264, 8), (1500, 1032, 0), (1030, 2048, 0)])
+                                        (2, 16400, 40), (1, 131056, 0), (1025, 264, 8), (1500, 1032, 0), (1030, 2048, 0),
+                                        (6500, 72, 0), (3200, 600, 8), (1700, 1480, 0), (1600, 2056, 0), (800, 4104, 8), (390, 8200, 0)])
 def test_quant_bit_for_bit(dtype, rows, C, pad):
     """Same formula, same IEEE roundings: values and scales are equal."""
     need_gpu()
@@ -252,7 +253,9 @@ def test_gemm_offsets_past_32_bits():
 # ------------------------------------------------------------------ between branches
 
 WIDTHS = [(1, 8, 1), (1, 2048, 1), (5, 136, 2), (7, 520, 3), (3, 1032, 3), (6, 1480, 4), (9, 4096, 3), (2, 8200, 1), (3, 16384, 2),
-          (1025, 256, 1000), (1500, 1032, 7), (1027, 2048, 400), (700, 4104, 9), (5000, 264, 1250)]
+          (1025, 256, 1000), (1500, 1032, 7), (1027, 2048, 400),
+          # more rows than there are walks, samples that end between a walk's rows
+          (6500, 264, 1250), (3200, 600, 999), (1700, 2048, 400), (800, 2056, 100), (700, 4104, 9), (400, 8200, 1)]
 
 
 @TYPES

@@ -91,11 +91,131 @@ __device__ __forceinline__ void epilogue(const GemmI8Args& a, int r0, int c0, in
   }
 }
 
+// ---------------------------------------------------------------- one and two rows
+// A wavefront takes R rows of W, 1024 bytes of one at a time, and multiplies them with the MR rows of A from LDS by
+// four-byte dot products; the lanes' sums meet by DPP.  Rows of A in a float type are put in 8 bits by every
+// workgroup for itself while its first pieces of W are on their way, which saves the launch that would do it once.
+// Bound by a launch, the latency of two dependent steps and W's bytes.  N = 8192, K = 2048 (16.8 MB), us, one row: 4.9,
+// bf16 rows 5.4; k_gemm_i8_dir 5.5, with a launch before it 7.5.  Two rows 5.3 (5.6), bf16 6.7 (7.7); four rows 6.4
+// (5.7), bf16 9.1 (7.7), so two at most.  N = 2048, K = 8192, one row 5.0 (7.2).
+__device__ __forceinline__ int lanes_sum(int v) {
+  v += __builtin_amdgcn_mov_dpp(v, 0xB1, 0xf, 0xf, false);    // quad_perm [1, 0, 3, 2]
+  v += __builtin_amdgcn_mov_dpp(v, 0x4E, 0xf, 0xf, false);    // quad_perm [2, 3, 0, 1]
+  v += __builtin_amdgcn_mov_dpp(v, 0x141, 0xf, 0xf, false);   // row_half_mirror
+  v += __builtin_amdgcn_mov_dpp(v, 0x140, 0xf, 0xf, false);   // row_mirror
+  const auto r16 = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
+  v = (int)(r16[0] + r16[1]);
+  const auto r32 = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
+  return (int)(r32[0] + r32[1]);
+}
+constexpr int kVecRows = 2, kVecBytes = 65536;   // rows, and bytes of A that a workgroup holds
+
+template <int DA, int DT, int MR, int R>
+__global__ __launch_bounds__(256) void k_gemm_i8_vec(GemmI8Args a) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t rows[];   // [MR][Kp]: zeros past K
+  __shared__ uint32_t tops[MR][4];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n0 = (blockIdx.x * 4 + wave) * R, steps = (a.K + 1023) / 1024, Kp = steps * 1024;
+  constexpr int G = 8 / R;   // steps at once: 8 loads in flight
+  u32x4_t w[G][R];
+  auto request = [&](int s0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int r = 0; r < R; ++r) {   // past K or N: the first row's start, which meets zeros or is not stored
+        const int k = (s0 + g) * 1024 + lane * 16;
+        if (s0 + g < steps) w[g][r] = *reinterpret_cast<const u32x4_t*>(a.w + (size_t)(n0 + r < a.N ? n0 + r : 0) * a.w_row + (k < a.K ? k : 0));
+      }
+  };
+  request(0);
+  // what the last step needs, requested now
+  const int om = lane / R, on = n0 + lane % R;   // the output that this lane finishes
+  const bool mine = om < a.M && om < MR && on < a.N;
+  float sa = 0.f, sw = 0.f, bias = 0.f, gate = 1.f, resid = 0.f;
+  if (mine) {
+    sw = a.w_s[on];
+    if (DA == DT_I8) sa = a.a_s[om];
+    if (a.bias) bias = St<DT>::ld1(a.bias, on);
+    if (a.gate) gate = a.gate[(size_t)(om / a.gate_rows) * a.gate_ld + on];
+    if (a.resid) resid = St<DT>::ld1(a.resid, (size_t)om * a.resid_row + on);
+  }
+  if constexpr (DA == DT_I8) {
+    for (int i = threadIdx.x * 16; i < MR * Kp; i += 4096) {
+      const int m = i / Kp, k = i - m * Kp;
+      u32x4_t x = {0, 0, 0, 0};
+      if (m < a.M && k < a.K) x = *reinterpret_cast<const u32x4_t*>(static_cast<const uint8_t*>(a.a) + (size_t)m * a.a_row + k);
+      *reinterpret_cast<u32x4_t*>(rows + i) = x;
+    }
+  } else {
+    uint32_t top[MR];
+#pragma unroll
+    for (int m = 0; m < MR; ++m) {
+      top[m] = 0;
+      for (int k = threadIdx.x * 8; m < a.M && k < a.K; k += 2048) {
+        float v[8];
+        load8<DA>(a.a, (size_t)m * a.a_row + k, v);
+        top[m] = top_bits<8>(v, top[m]);
+      }
+      top[m] = top64(top[m]);
+      if (lane == 0) tops[m][wave] = top[m];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int m = 0; m < MR; ++m) {
+      const I8Scale q(max(max(tops[m][0], tops[m][1]), max(tops[m][2], tops[m][3])));
+      if (om == m) sa = q.s;
+      for (int k = threadIdx.x * 8; k < Kp; k += 2048) {
+        u32x2_t x = {0, 0};
+        if (m < a.M && k < a.K) {
+          float v[8];
+          load8<DA>(a.a, (size_t)m * a.a_row + k, v);   // from the caches
+          x = i8_pack8(v, q);
+        }
+        *reinterpret_cast<u32x2_t*>(rows + m * Kp + k) = x;
+      }
+    }
+  }
+  __syncthreads();
+  int acc[MR][R];
+#pragma unroll
+  for (int m = 0; m < MR; ++m)
+#pragma unroll
+    for (int r = 0; r < R; ++r) acc[m][r] = 0;
+  for (int s0 = 0; s0 < steps; s0 += G) {
+    if (s0) request(s0);
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      if (s0 + g >= steps) break;
+#pragma unroll
+      for (int m = 0; m < MR; ++m) {
+        const u32x4_t x = *reinterpret_cast<const u32x4_t*>(rows + m * Kp + (s0 + g) * 1024 + lane * 16);
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[m][r] = __builtin_amdgcn_sdot4((int)w[g][r][e], (int)x[e], acc[m][r], false);
+      }
+    }
+  }
+  float v = 0.f;
+#pragma unroll
+  for (int m = 0; m < MR; ++m)
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int s = lanes_sum(acc[m][r]);
+      if (lane == m * R + r) v = (float)s;
+    }
+  if (!mine) return;
+  v = v * sa * sw + bias;
+  if (a.gelu) v = gelu_tanh_f(v);
+  St<DT>::st1(a.out, (size_t)om * a.out_row + on, v * gate + resid);
+}
+
 // Few rows: 16 x 16 tile, operands straight from memory, the NW waves of a workgroup on interleaved blocks of 128 k;
-// their sums meet in LDS.
+// their sums meet in LDS.  Bound by the latency of the loads: M = 16, N = 8192, K = 2048 6.4 us; groups of four blocks
+// whatever is left, the rest clamped to the row's start, took 9.9.  16 waves were no faster (7.4; N = 2048,
+// K = 8192 9.8 for 9.7).
 template <int DT, int NW>
 __global__ __launch_bounds__(NW * 64) void k_gemm_i8_dir(GemmI8Args a) {
-  constexpr int U = 4;
   __shared__ i32x4_t red[NW][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, g = lane >> 4;
@@ -105,7 +225,9 @@ __global__ __launch_bounds__(NW * 64) void k_gemm_i8_dir(GemmI8Args a) {
   const uint8_t* pw = a.w + (size_t)n * a.w_row;
   i32x4_t acc = {0, 0, 0, 0};
   const int nk = (a.K + kQBlock - 1) / kQBlock;
-  for (int b0 = wave; b0 < nk; b0 += NW * U) {
+  // U of the wave's blocks at once: their loads are all on their way before the first product
+  auto blocks = [&](int b0, auto Uc) __attribute__((always_inline)) {
+    constexpr int U = decltype(Uc)::value;
     u32x4_t x[U][2], w[U][2];
 #pragma unroll
     for (int u = 0; u < U; ++u)
@@ -124,7 +246,11 @@ __global__ __launch_bounds__(NW * 64) void k_gemm_i8_dir(GemmI8Args a) {
         for (int e = 0; e < 4; ++e) w[u][h][e] = on ? w[u][h][e] : 0u;
         acc = mfma_i8(w[u][h], x[u][h], acc);
       }
-  }
+  };
+  int b0 = wave;
+  for (; b0 + 3 * NW < nk; b0 += 4 * NW) blocks(b0, Int<4>{});
+  for (; b0 + NW < nk; b0 += 2 * NW) blocks(b0, Int<2>{});
+  if (b0 < nk) blocks(b0, Int<1>{});
   red[wave][lane] = acc;
   __syncthreads();
   if (wave) return;
@@ -556,8 +682,16 @@ size_t rows_bytes(int a_dtype, int M, int K) { return a_dtype == DT_I8 ? 0 : ((s
 
 }  // namespace
 
-// The kernel of a shape by estimated time (us)
+// The kernel of a shape by estimated time (us), as 8-bit rows measured over 60 shapes of 1 to 14566 rows, N and K of 256 to
+// 8192 (bf16 out).  A tile of 64 x 64 takes 0.21 us per block of K while each CU has one, 0.5 with two on every
+// CU; 128 x 128 0.42 alone, 0.71 with all CUs (what the caches deliver); 256 x 256 1.65.  Splits of K add the join:
+// a launch, and writing and reading the partial sums.
+//   M 64 N 2048 K 2048: 16 x 16 5.6 us, 64 x 64 5.7; M 128 N 2048: 64 x 64 5.8 (16 x 16 16); M 16 N 8192: 6.4, 6.8
+//   M 64 N 2048 K 8192: 64 x 64 14.4 us, with 2 / 4 / 8 splits 12.5 / 11.1 / 12.6; 16 x 16 16.6
+//   M 512 N 8192 K 2048: 128 x 128 12.9 us, 64 x 64 17.0, 256 x 256 25.1
+//   M 4608 N 6144 K 2048: 256 x 256 59.0 us, 128 x 128 77.7, 64 x 64 97.0
 I8Plan gemm_i8_plan(int out_dtype, int M, int N, int K) {
+  if (M <= kVecRows && (size_t)M * ((K + 1023) / 1024 * 1024) <= kVecBytes) return I8Plan{I8_VEC, 1};
   const int nk = (K + kQBlock - 1) / kQBlock;
   // us per block of K: few tiles, what 256 tiles add, and a round of all CUs (512 tiles of 64 x 64)
   const double c6[3] = {0.21, 0.08, 0.50}, c12[3] = {0.42, 0.30, 0.71};
@@ -574,7 +708,7 @@ I8Plan gemm_i8_plan(int out_dtype, int M, int N, int K) {
     if (s > 1 && nk / s < 8) break;
     const double t = (double)tiles(M, N, 64) * s, nb = (double)nk / s;
     const double main = t <= 256 ? (c6[0] + c6[1] * t / 256) * nb : ceil(t / 512) * c6[2] * nb;
-    take(I8_TILE64, s, 3.5 + main + (s > 1 ? 1.8 + s * (0.35 + 2.3e-6 * M * N) : 0.0));
+    take(I8_TILE64, s, 3.5 + main + (s > 1 ? 2.4 + s * (0.35 + 2.3e-6 * M * N) : 0.0));
   }
   const double t128 = (double)tiles(M, N, 128), t256 = (double)tiles(M, N, 256);
   take(I8_TILE128, 1, 3.5 + (t128 <= 256 ? c12[0] + c12[1] * t128 / 256 : ceil(t128 / 256) * c12[2]) * nk);
@@ -583,6 +717,14 @@ I8Plan gemm_i8_plan(int out_dtype, int M, int N, int K) {
 }
 
 namespace {
+
+template <int DA, int DT>
+void launch_vec(const GemmI8Args& a, hipStream_t s) {
+  const size_t lds = (size_t)a.M * ((a.K + 1023) / 1024 * 1024);
+  const unsigned wg = (unsigned)((a.N + 7) / 8);
+  if (a.M == 1) FF_LAUNCH((k_gemm_i8_vec<DA, DT, 1, 2>), wg, 256, lds, s, a);
+  else FF_LAUNCH((k_gemm_i8_vec<DA, DT, 2, 2>), wg, 256, lds, s, a);
+}
 
 template <int DT>
 hipError_t launch_i8(const GemmI8Args& a, const I8Plan& p, hipStream_t s) {
@@ -603,7 +745,9 @@ hipError_t launch_i8(const GemmI8Args& a, const I8Plan& p, hipStream_t s) {
 
 size_t gemm_i8_workspace(int a_dtype, int out_dtype, int M, int N, int K) {
   if (M <= 0) return 0;
-  const int n = gemm_i8_plan(out_dtype, M, N, K).splits;
+  const I8Plan p = gemm_i8_plan(out_dtype, M, N, K);
+  if (p.kernel == I8_VEC) return 0;
+  const int n = p.splits;
   return rows_bytes(a_dtype, M, K) + (n > 1 ? (size_t)n * M * N * 4 : 0);
 }
 
@@ -611,6 +755,13 @@ hipError_t gemm_i8(int a_dtype, int out_dtype, const GemmI8Args& a0, hipStream_t
   if (a0.M <= 0) return hipSuccess;
   const I8Plan p = gemm_i8_plan(out_dtype, a0.M, a0.N, a0.K);
   GemmI8Args a = a0;
+  if (p.kernel == I8_VEC) {
+    const bool b = out_dtype == DT_BF16;
+    if (a_dtype == DT_I8) b ? launch_vec<DT_I8, DT_BF16>(a, s) : launch_vec<DT_I8, DT_F32>(a, s);
+    else if (a_dtype == DT_BF16) b ? launch_vec<DT_BF16, DT_BF16>(a, s) : launch_vec<DT_BF16, DT_F32>(a, s);
+    else b ? launch_vec<DT_F32, DT_BF16>(a, s) : launch_vec<DT_F32, DT_F32>(a, s);
+    return hipGetLastError();
+  }
   if (a_dtype != DT_I8) {
     uint8_t* const q = reinterpret_cast<uint8_t*>(a0.part);
     float* const qs = reinterpret_cast<float*>(q + ((size_t)a.M * a.K + 255) / 256 * 256);

@@ -221,7 +221,7 @@ struct GemmI8Args {
 constexpr int kI8MaxK = 131056;   // K * 128 * 128 < 2^31: sums of products stay within 32 bits
 enum { DT_I8 = 2 };
 // What a shape is run with: a kernel (its tile), and workgroups that share a tile's K
-enum { I8_DIR, I8_TILE64, I8_TILE128, I8_TILE256 };
+enum { I8_DIR, I8_TILE64, I8_TILE128, I8_TILE256, I8_VEC };
 struct I8Plan { int kernel, splits; };
 I8Plan gemm_i8_plan(int out_dtype, int M, int N, int K);
 size_t gemm_i8_workspace(int a_dtype, int out_dtype, int M, int N, int K);

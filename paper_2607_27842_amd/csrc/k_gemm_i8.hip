@@ -25,32 +25,39 @@ __device__ __forceinline__ i32x16_t mfma_i8(u32x4_t a, u32x4_t b, i32x16_t c) {
 }
 
 // ---------------------------------------------------------------- epilogue
-// Bias, activation and gate of 8 columns c.. of row r, on the sums times both scales
+// Activation and gate of 8 columns c.. of row r, on the sums times both scales and the bias
 template <int DT>
-__device__ __forceinline__ void act_gate(const GemmI8Args& a, int r, int c, const float* bias, float (&v)[8]) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] += bias[e];
+__device__ __forceinline__ void act_gate(const GemmI8Args& a, int r, int c, float (&v)[8]) {
   if (a.gelu) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = gelu_tanh_f(v[e]);
   }
   if (a.gate) {
     float g[8];
-    load8<DT_F32>(a.gate, (size_t)((uint32_t)r / (uint32_t)a.gate_rows) * a.gate_ld + c, g);
+    load8<DT_F32>(a.gate, (size_t)((uint32_t)(r + a.row0) / (uint32_t)a.gate_rows) * a.gate_ld + c, g);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] *= g[e];
   }
 }
 
+// Word of a row's 4 columns col .. col + 3 in a wave's LDS region: rows of WN words, their 16-byte chunks in an order of the
+// row's own (WN = 64), or four words more a row; 16 rows' same chunk then lies in 16 different sets of banks.
+template <int WN>
+__device__ __forceinline__ int sum_at(int row, int col) {
+  if constexpr (WN == 64) return row * WN + (((col >> 2) ^ (row & 15)) << 2);
+  else return row * (WN + 4) + col;
+}
+template <int WN> constexpr int sum_words(int rows) { return rows * (WN == 64 ? WN : WN + 4); }
+
 // Rows r0 .. r0 + RB NB - 1, columns c0 .. c0 + WN - 1 of a wavefront: put(i) lays RB rows of sums at a time into
-// the wave's own LDS region, a row every WN + 4 words, and they come back as 8-column pieces, so that
+// the wave's own LDS region, and they come back as 8-column pieces, so that
 // every load and store of bias, gate, residual and output is 16 bytes wide and covers whole row segments (in
 // the MFMA layout each store would put 8 bytes into each of 16 or 32 rows).  N % 8 == 0: a piece is in range as
 // a whole.  The caller has retired all waves' reads of what the region overlays.
 template <int DT, int WN, int RB, int NB, class F>
 __device__ __forceinline__ void epilogue(const GemmI8Args& a, int r0, int c0, int* lds, F&& put) {
-  constexpr int LDW = WN + 4, CPR = WN / 8, RPP = 64 / CPR, NPASS = RB / RPP;
-  static_assert(64 % CPR == 0 && NPASS >= 1, "whole rows a pass");
+  constexpr int CPR = WN / 8, RPP = 64 / CPR, NPASS = RB / RPP;
+  static_assert(64 % CPR == 0 && NPASS >= 1 && 64 % RPP == 0, "whole rows a pass, passes within 64 rows");
   const int lane = threadIdx.x & 63;
   const int pc = lane % CPR * 8, pr = lane / CPR, c = c0 + pc;
   const int cl = c < a.N ? c : 0;   // loads past the matrix read its first column or last row
@@ -59,32 +66,40 @@ __device__ __forceinline__ void epilogue(const GemmI8Args& a, int r0, int c0, in
   for (int e = 0; e < 8; ++e) bias[e] = 0.f;
   if (a.bias) load8<DT>(a.bias, cl, bias);
   load8<DT_F32>(a.w_s, cl, sw);
-  // the rows' scales and the residual's pieces are requested a block ahead
+  // All rows' scales are read first, one a lane: a load between the stores would be waited for behind the stores before
+  // it.  The residual's pieces are requested a block ahead.
+  constexpr int NS = (RB * NB + 63) / 64;
+  float sa[NS];
+#pragma unroll
+  for (int i = 0; i < NS; ++i) sa[i] = a.a_s[min(r0 + 64 * i + lane, a.M - 1)];
   typedef typename Raw8<DT>::type raw_t;
   raw_t res[2][NPASS];
-  float sa[2][NPASS];
   auto request = [&](int i) __attribute__((always_inline)) {
+    if (a.resid) {
 #pragma unroll
-    for (int p = 0; p < NPASS; ++p) {
-      const int r = min(r0 + i * RB + p * RPP + pr, a.M - 1);
-      sa[i & 1][p] = a.a_s[r];
-      if (a.resid) res[i & 1][p] = Raw8<DT>::load(a.resid, (size_t)r * a.resid_row + cl);
+      for (int p = 0; p < NPASS; ++p)
+        res[i & 1][p] = Raw8<DT>::load(a.resid, (size_t)min(r0 + i * RB + p * RPP + pr, a.M - 1) * a.resid_row + cl);
     }
   };
   request(0);
 #pragma unroll
   for (int i = 0; i < NB; ++i) {
+    // lanes read what other lanes wrote: to the compiler, too, the region changes here
+    asm volatile("" ::: "memory");
     put(i);
+    asm volatile("" ::: "memory");
     if (i + 1 < NB) request(i + 1);
 #pragma unroll
     for (int p = 0; p < NPASS; ++p) {
       const int r = r0 + i * RB + p * RPP + pr;
-      const i32x4_t x0 = *reinterpret_cast<const i32x4_t*>(lds + (p * RPP + pr) * LDW + pc);
-      const i32x4_t x1 = *reinterpret_cast<const i32x4_t*>(lds + (p * RPP + pr) * LDW + pc + 4);
+      const i32x4_t x0 = *reinterpret_cast<const i32x4_t*>(lds + sum_at<WN>(p * RPP + pr, pc));
+      const i32x4_t x1 = *reinterpret_cast<const i32x4_t*>(lds + sum_at<WN>(p * RPP + pr, pc + 4));
+      const int ri = i * RB + p * RPP;   // + pr, below 64 more than the multiple of 64 that it lies behind
+      const float sr = __shfl(sa[ri / 64], ri % 64 + pr, 64);
       float v[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = (float)(e < 4 ? x0[e & 3] : x1[e & 3]) * sa[i & 1][p] * sw[e];
-      act_gate<DT>(a, min(r, a.M - 1), cl, bias, v);
+      for (int e = 0; e < 8; ++e) v[e] = fmaf((float)(e < 4 ? x0[e & 3] : x1[e & 3]) * sr, sw[e], bias[e]);
+      act_gate<DT>(a, min(r, a.M - 1), cl, v);
       if (a.resid) Raw8<DT>::add(res[i & 1][p], v);
       if (r < a.M && c < a.N) store8<DT>(a.out, (size_t)r * a.out_row + c, v);
     }
@@ -268,7 +283,7 @@ __global__ __launch_bounds__(NW * 64) void k_gemm_i8_dir(GemmI8Args a) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = gelu_tanh_f(v[e]);
   }
-  if (a.gate) v *= load4<DT_F32>(a.gate, (size_t)(r / a.gate_rows) * a.gate_ld + c);
+  if (a.gate) v *= load4<DT_F32>(a.gate, (size_t)((r + a.row0) / a.gate_rows) * a.gate_ld + c);
   if (a.resid) v += load4<DT>(a.resid, (size_t)r * a.resid_row + c);
   const size_t o = (size_t)r * a.out_row + c;
   if (DT == DT_BF16) *reinterpret_cast<u32x2_t*>(reinterpret_cast<uint16_t*>(a.out) + o) = u32x2_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
@@ -287,6 +302,12 @@ __global__ __launch_bounds__(NW * 64) void k_gemm_i8_dir(GemmI8Args a) {
 // and reads: phase 0 all B and A0 of stage k, phases 1-3 A1-A3.  So a piece's slot is refilled no earlier than
 // one phase after its last read.
 // K % 128 != 0: the last stage's chunks past K are out of the resource's range and load zeros.
+// What bounds it: with random operands the card's power limit (the same cycles on zeros, at a higher clock, take 0.65 of the
+// time at K = 8192, where MFMAs are busy 73 % of the cycles), then the epilogue, which one workgroup a CU leaves
+// uncovered.  M = 14336, N = 8192, K = 2048 (7 rounds of 256 tiles) 230 us, 2.09 POP/s, with bias and GELU 260; 210
+// and 231 without the stores (a measurement only); 8192 x 8192 x 8192 441 us, 2.49 POP/s.  A workgroup that walks
+// over tiles and requests the next one's first stages before its epilogue took 240 us: its stores hold the waits for the
+// next tile's operands.
 constexpr int kPPIssue[4][3] = {{3, -1, -1}, {0, 4, 5}, {1, 6, -1}, {2, 7, -1}};   // A0-A3, B0-B3
 // How many of a wave's DMAs may be outstanding at the end of phase p of a stage with `left` stages
 // after it (2: two or more), so that what phase p + 1 reads has landed.
@@ -310,7 +331,7 @@ __global__ __launch_bounds__(512) void k_gemm_i8_pp(GemmI8Args a) {
 #ifdef __HIP_DEVICE_COMPILE__   // the host pass needs the launch stub only
   constexpr int BM = 256, BN = 256, TN = 4, WN = 16 * TN, RB = kQBlock;   // RB: bytes of an LDS row
   constexpr int PC = 64 * RB, BUFA = 4 * PC, BUFB = TN * PC, OFFB = 2 * BUFA;
-  constexpr int kMain = OFFB + 2 * BUFB, kEpi = 8 * 32 * (WN + 4) * 4;
+  constexpr int kMain = OFFB + 2 * BUFB, kEpi = 8 * sum_words<WN>(32) * 4;
   __shared__ __attribute__((aligned(1024))) char lds[kMain > kEpi ? kMain : kEpi];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int tm, tn;
@@ -462,14 +483,14 @@ __global__ __launch_bounds__(512) void k_gemm_i8_pp(GemmI8Args a) {
 #undef FF_RDA
 #undef FF_MMA
   // every wave's LDS reads and DMA ended before the last barrier
-  int* const own = reinterpret_cast<int*>(lds) + wave * 32 * (WN + 4);
+  int* const own = reinterpret_cast<int*>(lds) + wave * sum_words<WN>(32);
   epilogue<DT, WN, 32, 4>(a, m0 + mw * 128, n0 + nw * WN, own, [&](int i) __attribute__((always_inline)) {
     // lane l: row l % 32, columns 8 j + 4 (l / 32) + 0..3
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        *reinterpret_cast<i32x4_t*>(own + fr * (WN + 4) + 32 * u + 8 * j + 4 * fh) =
+        *reinterpret_cast<i32x4_t*>(own + sum_at<WN>(fr, 32 * u + 8 * j + 4 * fh)) =
             i32x4_t{acc[i][u][4 * j], acc[i][u][4 * j + 1], acc[i][u][4 * j + 2], acc[i][u][4 * j + 3]};
   });
 #endif
@@ -481,6 +502,8 @@ __global__ __launch_bounds__(512) void k_gemm_i8_pp(GemmI8Args a) {
 // Per block a wave has a memory slot (its fragments) and a matrix slot (the MFMAs, and behind each a DMA of the block
 // NS ahead into the ring slot just read), each ended by a barrier; the second group runs one slot
 // behind, one wave of each group per SIMD.  The two groups' sums meet in LDS: each finishes half of the rows.
+// What bounds it: the chain of LDS reads, waits and barriers (64 x 64: 0.17 us a block of K with one workgroup on a CU, 0.36
+// a pair of blocks with two), and with all CUs what the caches deliver (128 x 128: 0.5 us a block).
 template <int DT, int BM, int BN, int NS>
 __global__ __launch_bounds__(512) void k_gemm_i8_two(GemmI8Args a, int splits) {
 #ifdef __HIP_DEVICE_COMPILE__   // the host pass needs the launch stub only
@@ -488,7 +511,7 @@ __global__ __launch_bounds__(512) void k_gemm_i8_two(GemmI8Args a, int splits) {
   constexpr int STB = (BM + BN) * RB;   // bytes of a block
   constexpr int NA = BM / 32, NW = BN / 32, PER = NA + NW;   // DMA instructions of a wave and block
   constexpr int kMain = 2 * NS * STB;
-  constexpr int HT = TM / 2, kXch = 8 * HT * TN * 1024, RE = HT > 1 ? 32 : 16, kEpi = kXch + 8 * RE * (WN + 4) * 4;
+  constexpr int HT = TM / 2, kXch = 8 * HT * TN * 1024, RE = HT > 1 ? 32 : 16, kEpi = kXch + 8 * sum_words<WN>(RE) * 4;
   static_assert(TM % 2 == 0 && PER <= 2 * TM * TN, "halves of the rows; a DMA behind an MFMA");
   __shared__ __attribute__((aligned(1024))) char lds[kMain > kEpi ? kMain : kEpi];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -634,12 +657,12 @@ __global__ __launch_bounds__(512) void k_gemm_i8_two(GemmI8Args a, int splits) {
       }
     return;
   }
-  int* const own = reinterpret_cast<int*>(lds + kXch) + wave * RE * (WN + 4);
+  int* const own = reinterpret_cast<int*>(lds + kXch) + wave * sum_words<WN>(RE);
   epilogue<DT, WN, RE, HT * 16 / RE>(a, r0, c0, own, [&](int i) __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < RE / 16; ++t)
 #pragma unroll
-      for (int j = 0; j < TN; ++j) *reinterpret_cast<i32x4_t*>(own + (16 * t + fr) * (WN + 4) + 16 * j + 4 * fh) = fin[i * (RE / 16) + t][j];
+      for (int j = 0; j < TN; ++j) *reinterpret_cast<i32x4_t*>(own + sum_at<WN>(16 * t + fr, 16 * j + 4 * fh)) = fin[i * (RE / 16) + t][j];
   });
 #endif
 }
@@ -659,13 +682,14 @@ __global__ __launch_bounds__(256) void k_gemm_i8_join(GemmI8Args a, int splits) 
   }
   float v[8], x[8];
   const float sa = a.a_s[r];
+  float bias[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) bias[e] = 0.f;
   load8<DT_F32>(a.w_s, c, x);
+  if (a.bias) load8<DT>(a.bias, c, bias);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = (float)s[e / 4][e % 4] * sa * x[e];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = 0.f;
-  if (a.bias) load8<DT>(a.bias, c, x);
-  act_gate<DT>(a, r, c, x, v);
+  for (int e = 0; e < 8; ++e) v[e] = fmaf((float)s[e / 4][e % 4] * sa, x[e], bias[e]);
+  act_gate<DT>(a, r, c, v);
   if (a.resid) {
     load8<DT>(a.resid, (size_t)r * a.resid_row + c, x);
 #pragma unroll
@@ -680,43 +704,62 @@ long tiles(long M, long N, long t) { return ((M + t - 1) / t) * ((N + t - 1) / t
 // rows that the call puts in 8 bits itself, and their scales behind them
 size_t rows_bytes(int a_dtype, int M, int K) { return a_dtype == DT_I8 ? 0 : ((size_t)M * K + 255) / 256 * 256 + ((size_t)M * 4 + 255) / 256 * 256; }
 
-}  // namespace
-
-// The kernel of a shape by estimated time (us), as 8-bit rows measured over 60 shapes of 1 to 14566 rows, N and K of 256 to
-// 8192 (bf16 out).  A tile of 64 x 64 takes 0.21 us per block of K while each CU has one, 0.5 with two on every
-// CU; 128 x 128 0.42 alone, 0.71 with all CUs (what the caches deliver); 256 x 256 1.65.  Splits of K add the join:
-// a launch, and writing and reading the partial sums.
-//   M 64 N 2048 K 2048: 16 x 16 5.6 us, 64 x 64 5.7; M 128 N 2048: 64 x 64 5.8 (16 x 16 16); M 16 N 8192: 6.4, 6.8
-//   M 64 N 2048 K 8192: 64 x 64 14.4 us, with 2 / 4 / 8 splits 12.5 / 11.1 / 12.6; 16 x 16 16.6
+// The kernel of a shape by estimated time (us): fits to 60 shapes of 1 to 14566 rows, N and K of 256 to 8192, 8-bit rows,
+// bf16 out.  nk: blocks of K; t: tiles.  Examples, measured:
+//   M 16 N 8192 K 2048: 16 x 16 6.4 us, 64 x 64 6.8; M 64 N 2048: 5.6, 5.7; M 128 N 2048: 16, 5.8
+//   M 64 N 2048 K 8192: 64 x 64 14.4 us, with 2 / 4 / 8 splits of K 12.5 / 11.1 / 12.6; 16 x 16 16.6
 //   M 512 N 8192 K 2048: 128 x 128 12.9 us, 64 x 64 17.0, 256 x 256 25.1
 //   M 4608 N 6144 K 2048: 256 x 256 59.0 us, 128 x 128 77.7, 64 x 64 97.0
-I8Plan gemm_i8_plan(int out_dtype, int M, int N, int K) {
-  if (M <= kVecRows && (size_t)M * ((K + 1023) / 1024 * 1024) <= kVecBytes) return I8Plan{I8_VEC, 1};
+double us_dir(double t, double nk) { return 2.2 + fmax(t * nk * 0.45e-3, 0.115 * nk); }
+double us_64(double t, double nk) {
+  if (t <= 256) return 3.5 + (0.17 + 0.06 * t / 256) * nk;
+  if (t <= 512) return 3.5 + (0.23 + 0.13 * (t - 256) / 256) * nk;
+  return 3.0 + t / 512 * (0.36 * nk + 1.3);
+}
+double us_join(int splits, double outputs) { return 1.2 + splits * (0.55 + 0.5e-6 * outputs); }
+double us_128(double t, double nk) { return t <= 256 ? 5.5 + (0.37 + 0.10 * t / 256) * nk : 3.0 + ceil(t / 256) * (0.5 * nk + 2.2); }
+// rounds of all 256 CUs run at the power limit, a last one with fewer at a higher clock
+double us_256(double t, double nk) {
+  const double full = floor(t / 256), last = t / 256 - full, f = last * last;
+  return 4.0 + full * (1.6 * nk + 6.5) + (last > 0 ? (0.95 + 0.65 * f) * nk + 1.0 + 5.5 * f : 0.0);
+}
+
+struct Timed { I8Plan plan; double us; };
+Timed best_of(int M, int N, int K, bool cut) {
   const int nk = (K + kQBlock - 1) / kQBlock;
-  // us per block of K: few tiles, what 256 tiles add, and a round of all CUs (512 tiles of 64 x 64)
-  const double c6[3] = {0.21, 0.08, 0.50}, c12[3] = {0.42, 0.30, 0.71};
-  I8Plan best{I8_TILE128, 1};
-  double least = 1e30;
-  auto take = [&](int k, int splits, double us) {
-    if (us < least) { least = us; best = I8Plan{k, splits}; }
+  const double t64 = (double)tiles(M, N, 64), t256 = (double)tiles(M, N, 256);
+  Timed b{{I8_TILE128, 1, M}, us_128((double)tiles(M, N, 128), nk)};
+  auto take = [&](int k, int splits, int head, double us) {
+    if (us < b.us) b = Timed{{k, splits, head}, us};
   };
-  if (M <= 256) {
-    const double t = (double)tiles(M, N, 16), chain = 0.4 * ((nk + 15) / 16);
-    take(I8_DIR, 1, 2.5 + (t * nk * 0.45e-3 > chain ? t * nk * 0.45e-3 : chain));
-  }
+  if (M <= 256) take(I8_DIR, 1, M, us_dir((double)tiles(M, N, 16), nk));
   for (int s = 1; s <= 8; s *= 2) {
     if (s > 1 && nk / s < 8) break;
-    const double t = (double)tiles(M, N, 64) * s, nb = (double)nk / s;
-    const double main = t <= 256 ? (c6[0] + c6[1] * t / 256) * nb : ceil(t / 512) * c6[2] * nb;
-    take(I8_TILE64, s, 3.5 + main + (s > 1 ? 2.4 + s * (0.35 + 2.3e-6 * M * N) : 0.0));
+    take(I8_TILE64, s, M, us_64(t64 * s, (double)nk / s) + (s > 1 ? us_join(s, (double)M * N) : 0.0));
   }
-  const double t128 = (double)tiles(M, N, 128), t256 = (double)tiles(M, N, 256);
-  take(I8_TILE128, 1, 3.5 + (t128 <= 256 ? c12[0] + c12[1] * t128 / 256 : ceil(t128 / 256) * c12[2]) * nk);
-  if (nk >= 3) take(I8_TILE256, 1, 4.0 + ceil(t256 / 256) * 1.75 * nk);
-  return best;
+  if (nk < 3) return b;
+  take(I8_TILE256, 1, M, us_256(t256, nk));
+  // Rows behind whole rounds of 256 x 256 tiles in a launch of their own, with the tile that suits them (M = 14566,
+  // N = 8192, K = 2048, whose eighth round has 32 tiles: 240 us for 257)
+  const int per = (N + 255) / 256;
+  const int head = (int)(floor(t256 / 256) * 256) / per * 256;
+  if (cut && head > 0 && head < M) take(I8_TILE256, 1, head, us_256((double)tiles(head, N, 256), nk) + best_of(M - head, N, K, false).us - 0.5);
+  return b;
+}
+
+}  // namespace
+
+I8Plan gemm_i8_plan(int out_dtype, int M, int N, int K) {
+  (void)out_dtype;
+  if (M <= kVecRows && (size_t)M * ((K + 1023) / 1024 * 1024) <= kVecBytes) return I8Plan{I8_VEC, 1, M};
+  return best_of(M, N, K, true).plan;
 }
 
 namespace {
+
+// The plan of the rows behind a plan's head
+I8Plan tail_plan(const I8Plan& p, int M, int N, int K) { return best_of(M - p.head, N, K, false).plan; }
+size_t part_bytes(const I8Plan& p, int M, int N) { return p.splits > 1 ? (size_t)p.splits * M * N * 4 : 0; }
 
 template <int DA, int DT>
 void launch_vec(const GemmI8Args& a, hipStream_t s) {
@@ -747,19 +790,18 @@ size_t gemm_i8_workspace(int a_dtype, int out_dtype, int M, int N, int K) {
   if (M <= 0) return 0;
   const I8Plan p = gemm_i8_plan(out_dtype, M, N, K);
   if (p.kernel == I8_VEC) return 0;
-  const int n = p.splits;
-  return rows_bytes(a_dtype, M, K) + (n > 1 ? (size_t)n * M * N * 4 : 0);
+  return rows_bytes(a_dtype, M, K) + (p.head < M ? part_bytes(tail_plan(p, M, N, K), M - p.head, N) : part_bytes(p, M, N));
 }
 
 hipError_t gemm_i8(int a_dtype, int out_dtype, const GemmI8Args& a0, hipStream_t s) {
   if (a0.M <= 0) return hipSuccess;
   const I8Plan p = gemm_i8_plan(out_dtype, a0.M, a0.N, a0.K);
+  const bool bf16 = out_dtype == DT_BF16;
   GemmI8Args a = a0;
   if (p.kernel == I8_VEC) {
-    const bool b = out_dtype == DT_BF16;
-    if (a_dtype == DT_I8) b ? launch_vec<DT_I8, DT_BF16>(a, s) : launch_vec<DT_I8, DT_F32>(a, s);
-    else if (a_dtype == DT_BF16) b ? launch_vec<DT_BF16, DT_BF16>(a, s) : launch_vec<DT_BF16, DT_F32>(a, s);
-    else b ? launch_vec<DT_F32, DT_BF16>(a, s) : launch_vec<DT_F32, DT_F32>(a, s);
+    if (a_dtype == DT_I8) bf16 ? launch_vec<DT_I8, DT_BF16>(a, s) : launch_vec<DT_I8, DT_F32>(a, s);
+    else if (a_dtype == DT_BF16) bf16 ? launch_vec<DT_BF16, DT_BF16>(a, s) : launch_vec<DT_BF16, DT_F32>(a, s);
+    else bf16 ? launch_vec<DT_F32, DT_BF16>(a, s) : launch_vec<DT_F32, DT_F32>(a, s);
     return hipGetLastError();
   }
   if (a_dtype != DT_I8) {
@@ -772,7 +814,22 @@ hipError_t gemm_i8(int a_dtype, int out_dtype, const GemmI8Args& a0, hipStream_t
     a.a_s = qs;
     a.part = reinterpret_cast<int*>(q + rows_bytes(a_dtype, a.M, a.K));
   }
-  return out_dtype == DT_BF16 ? launch_i8<DT_BF16>(a, p, s) : launch_i8<DT_F32>(a, p, s);
+  if (p.head < a.M) {
+    GemmI8Args h = a;
+    h.M = p.head;
+    const hipError_t e = bf16 ? launch_i8<DT_BF16>(h, p, s) : launch_i8<DT_F32>(h, p, s);
+    if (e != hipSuccess) return e;
+    const size_t es = dsize(out_dtype), at = (size_t)p.head;
+    const I8Plan tail = tail_plan(p, a.M, a.N, a.K);
+    a.a = static_cast<const uint8_t*>(a.a) + at * a.a_row;
+    a.a_s += at;
+    a.out = static_cast<char*>(a.out) + at * a.out_row * es;
+    if (a.resid) a.resid = static_cast<const char*>(a.resid) + at * a.resid_row * es;
+    a.row0 = p.head;
+    a.M -= p.head;
+    return bf16 ? launch_i8<DT_BF16>(a, tail, s) : launch_i8<DT_F32>(a, tail, s);
+  }
+  return bf16 ? launch_i8<DT_BF16>(a, p, s) : launch_i8<DT_F32>(a, p, s);
 }
 
 }  // namespace ff

@@ -217,12 +217,14 @@ struct GemmI8Args {
   void* out; int64_t out_row;
   int M, N, K, gelu;
   int* part;   // workspace: gemm_i8_workspace bytes
+  int row0;    // what gate counts its rows from: the matrix's row that stands first here
 };
 constexpr int kI8MaxK = 131056;   // K * 128 * 128 < 2^31: sums of products stay within 32 bits
 enum { DT_I8 = 2 };
-// What a shape is run with: a kernel (its tile), and workgroups that share a tile's K
+// What a shape is run with: a kernel (its tile), workgroups that share a tile's K, and the rows it takes (fewer than all:
+// the rest follow in a launch of their own)
 enum { I8_DIR, I8_TILE64, I8_TILE128, I8_TILE256, I8_VEC };
-struct I8Plan { int kernel, splits; };
+struct I8Plan { int kernel, splits, head; };
 I8Plan gemm_i8_plan(int out_dtype, int M, int N, int K);
 size_t gemm_i8_workspace(int a_dtype, int out_dtype, int M, int N, int K);
 hipError_t gemm_i8(int a_dtype, int out_dtype, const GemmI8Args& a, hipStream_t s);

@@ -331,7 +331,7 @@ ff_status ff_gemm_i8(const ff_gemm_i8_desc* d, const void* a, const float* a_s, 
   }
   CHECK(!eo.meets(ew), FF_E_SHAPE, "out overlaps the workspace");
   const GemmI8Args g{a, d->a_row, a_s, (const uint8_t*)w, d->w_row, w_s, bias, resid, d->resid_row, gate, d->gate_ld, d->gate_rows,
-                     out, d->out_row, d->M, d->N, d->K, d->gelu, need ? (int*)ws : nullptr};
+                     out, d->out_row, d->M, d->N, d->K, d->gelu, need ? (int*)ws : nullptr, 0};
   HIP_TRY(gemm_i8(d->a_dtype, d->out_dtype, g, reinterpret_cast<hipStream_t>(stream)), "8-bit integer gemm");
   return ok();
 }

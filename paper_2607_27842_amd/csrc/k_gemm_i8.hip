@@ -708,15 +708,19 @@ size_t rows_bytes(int a_dtype, int M, int K) { return a_dtype == DT_I8 ? 0 : ((s
 // bf16 out.  nk: blocks of K; t: tiles.  Examples, measured:
 //   M 16 N 8192 K 2048: 16 x 16 6.4 us, 64 x 64 6.8; M 64 N 2048: 5.6, 5.7; M 128 N 2048: 16, 5.8
 //   M 64 N 2048 K 8192: 64 x 64 14.4 us, with 2 / 4 / 8 splits of K 12.5 / 11.1 / 12.6; 16 x 16 16.6
+//   M 256 N 6144 K 2048: 64 x 128 9.0 us, 128 x 64 9.0, 64 x 64 9.8, 128 x 128 11.9; M 1024 N 2048 K 8192: 21.7, 22.4, 26.3, 28.6
 //   M 512 N 8192 K 2048: 128 x 128 12.9 us, 64 x 64 17.0, 256 x 256 25.1
 //   M 4608 N 6144 K 2048: 256 x 256 59.0 us, 128 x 128 77.7, 64 x 64 97.0
 double us_dir(double t, double nk) { return 2.2 + fmax(t * nk * 0.45e-3, 0.115 * nk); }
 double us_64(double t, double nk) {
   if (t <= 256) return 3.5 + (0.17 + 0.06 * t / 256) * nk;
-  if (t <= 512) return 3.5 + (0.23 + 0.13 * (t - 256) / 256) * nk;
-  return 3.0 + t / 512 * (0.36 * nk + 1.3);
+  if (t <= 512) return 4.3 + (0.30 + 0.04 * (t - 256) / 256) * nk;   // two workgroups on some CUs
+  return 3.0 + ceil(t / 256) / 2 * (0.36 * nk + 1.3);
 }
 double us_join(int splits, double outputs) { return 1.2 + splits * (0.55 + 0.5e-6 * outputs); }
+double us_64x128(double t, double nk) {
+  return t <= 256 ? 3.8 + t / 256 + (0.235 + 0.05 * t / 256) * nk : 3.0 + ceil(t / 256) * (0.285 * nk + 2.4);
+}
 double us_128(double t, double nk) { return t <= 256 ? 5.5 + (0.37 + 0.10 * t / 256) * nk : 3.0 + ceil(t / 256) * (0.5 * nk + 2.2); }
 // rounds of all 256 CUs run at the power limit, a last one with fewer at a higher clock
 double us_256(double t, double nk) {
@@ -737,6 +741,7 @@ Timed best_of(int M, int N, int K, bool cut) {
     if (s > 1 && nk / s < 8) break;
     take(I8_TILE64, s, M, us_64(t64 * s, (double)nk / s) + (s > 1 ? us_join(s, (double)M * N) : 0.0));
   }
+  take(I8_TILE64x128, 1, M, us_64x128((double)((M + 63) / 64) * ((N + 127) / 128), nk));
   if (nk < 3) return b;
   take(I8_TILE256, 1, M, us_256(t256, nk));
   // Rows behind whole rounds of 256 x 256 tiles in a launch of their own, with the tile that suits them (M = 14566,
@@ -774,6 +779,7 @@ hipError_t launch_i8(const GemmI8Args& a, const I8Plan& p, hipStream_t s) {
   switch (p.kernel) {
     case I8_DIR: FF_LAUNCH((k_gemm_i8_dir<DT, 8>), (unsigned)tiles(a.M, a.N, 16), 512, 0, s, a); break;
     case I8_TILE64: FF_LAUNCH((k_gemm_i8_two<DT, 64, 64, 2>), (unsigned)(tiles(a.M, a.N, 64) * p.splits), 512, 0, s, a, p.splits); break;
+    case I8_TILE64x128: FF_LAUNCH((k_gemm_i8_two<DT, 64, 128, 2>), (unsigned)((a.M + 63) / 64) * (unsigned)((a.N + 127) / 128), 512, 0, s, a, 1); break;
     case I8_TILE128: FF_LAUNCH((k_gemm_i8_two<DT, 128, 128, 2>), (unsigned)tiles(a.M, a.N, 128), 512, 0, s, a, 1); break;
     case I8_TILE256: FF_LAUNCH((k_gemm_i8_pp<DT>), (unsigned)tiles(a.M, a.N, 256), 512, 0, s, a); break;
   }

@@ -223,7 +223,7 @@ constexpr int kI8MaxK = 131056;   // K * 128 * 128 < 2^31: sums of products stay
 enum { DT_I8 = 2 };
 // What a shape is run with: a kernel (its tile), workgroups that share a tile's K, and the rows it takes (fewer than all:
 // the rest follow in a launch of their own)
-enum { I8_DIR, I8_TILE64, I8_TILE128, I8_TILE256, I8_VEC };
+enum { I8_DIR, I8_TILE64, I8_TILE64x128, I8_TILE128, I8_TILE256, I8_VEC };
 struct I8Plan { int kernel, splits, head; };
 I8Plan gemm_i8_plan(int out_dtype, int M, int N, int K);
 size_t gemm_i8_workspace(int a_dtype, int out_dtype, int M, int N, int K);

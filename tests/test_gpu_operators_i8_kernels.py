@@ -1,0 +1,74 @@
+"""Each kernel of the integer products at the sizes where its loops wrap and end, against 64 bits."""
+import math
+
+import pytest
+import torch
+
+import i8_plan_util as P
+import i8_util as I
+import op_util as O
+from gpu_util import need_gpu
+
+pytestmark = pytest.mark.gpu
+BF, F32, I8 = torch.bfloat16, torch.float32, torch.int8
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("rows", ["i8", "float"])
+@pytest.mark.parametrize("shape,plan", P.PRODUCTS)
+def test_products_by_kernel(dtype, rows, shape, plan):
+    """Bias, gate vectors whose rows end inside tiles and launches, residual.  The rows compared: the first 150, 100 around
+    each change of gate or launch, the last 150."""
+    need_gpu()
+    M, N, K = shape
+    assert P.product(M, N, K) == plan
+    g = O.gen(M + N + K)
+    a = torch.randint(-128, 128, (M, K), generator=g).to(I8)
+    w = torch.randint(-128, 128, (N, K), generator=g).to(I8)
+    a_s, w_s = torch.exp(O.randn((M,), g)), torch.exp(O.randn((N,), g)) / 1e5
+    b, r = O.randn((N,), g, dtype), O.randn((M, N), g, dtype)
+    per = max(1, 2 * M // 5 - 3)
+    gate = O.randn((-(-M // per), N), g)
+    out = torch.full((M, N + 8), 77.0, device="cuda").to(dtype)
+    if rows == "i8":
+        I.gemm_call(a.cuda(), a_s.cuda(), w.cuda(), w_s.cuda(), b.cuda(), False, gate.cuda(), per, r.cuda(), dtype, out[:, :N])
+    else:
+        x = (a.float() * a_s[:, None]).to(dtype)
+        I.gemm_call(x.cuda(), None, w.cuda(), w_s.cuda(), b.cuda(), False, gate.cuda(), per, r.cuda(), dtype, out[:, :N])
+    assert (out[:, N:] == 77.0).all()
+    near = torch.zeros(M, dtype=torch.bool)
+    for at in [0, M, plan[2]] + list(range(per, M, per)):
+        near[max(0, at - (150 if at == M else 50)):at + (150 if at == 0 else 50)] = True
+    pick = near.nonzero().flatten()
+    q, s = (a[pick], a_s[pick]) if rows == "i8" else I.quantise(x[pick])
+    ref, tol = I.gemm_ref(q, s, w, w_s, b, False, gate[pick // per], 1, r[pick], dtype)
+    O.close(out[:, :N][pick.cuda()], ref, tol, "gemm")
+    # the other rows, by their sums: the integers' exact row sums times the columns that share a gate and scale of one
+    one = torch.ones(N, device="cuda")
+    plain = I.gemm_call(a.cuda(), torch.ones(M, device="cuda"), w.cuda(), one, dtype=F32)
+    total = plain.double().sum(1).cpu()
+    want = (a.long() * w.long().sum(0)).sum(1).double()
+    # each of a row's N results is rounded once to 24 bits: at most 2^-24 of its magnitude
+    assert ((total - want).abs() <= 2.0 ** -24 * (plain.double().abs().sum(1).cpu()) + 1e-6).all()
+
+
+@pytest.mark.parametrize("K", [400, 2064])
+def test_two_streams_at_once(K):
+    """Calls on two streams with workspaces of their own, shared operands."""
+    need_gpu()
+    g = O.gen(3)
+    M, N = 260, 2056
+    x = O.randn((M, K), g, BF).cuda()
+    w, w_s = I.quantise(O.randn((N, K), g, std=1 / math.sqrt(K)))
+    w, w_s = w.cuda(), w_s.cuda()
+    want = I.gemm_call(x, None, w, w_s)
+    outs, sides = [torch.zeros_like(want) for _ in range(2)], [torch.cuda.Stream() for _ in range(2)]
+    n = 1 << 24
+    ws = [torch.empty(n, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for o, s, k in zip(outs, sides, ws):
+            with torch.cuda.stream(s):
+                I.gemm_call(x, None, w, w_s, out=o, ws=k)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], want) and torch.equal(outs[1], want)

@@ -23,14 +23,15 @@ template <int CTL>
 __device__ __forceinline__ uint32_t dpp_max(uint32_t x) {
   return max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, CTL, 0xf, 0xf, false));
 }
-// over 8 neighbouring lanes, over the wavefront; every lane receives it
-__device__ __forceinline__ uint32_t top8(uint32_t x) {
+// over 16 neighbouring lanes, over the wavefront; every lane receives it
+__device__ __forceinline__ uint32_t top16(uint32_t x) {
   x = dpp_max<0xB1>(x);      // quad_perm [1, 0, 3, 2]
   x = dpp_max<0x4E>(x);      // quad_perm [2, 3, 0, 1]
-  return dpp_max<0x141>(x);  // row_half_mirror
+  x = dpp_max<0x141>(x);     // row_half_mirror
+  return dpp_max<0x140>(x);  // row_mirror
 }
 __device__ __forceinline__ uint32_t top64(uint32_t x) {
-  x = dpp_max<0x140>(top8(x));   // row_mirror
+  x = top16(x);
   const auto r16 = __builtin_amdgcn_permlane16_swap(x, x, false, false);
   x = max((uint32_t)r16[0], (uint32_t)r16[1]);
   const auto r32 = __builtin_amdgcn_permlane32_swap(x, x, false, false);

@@ -225,6 +225,25 @@ __global__ __launch_bounds__(256) void k_gemm_i8_vec(GemmI8Args a) {
   St<DT>::st1(a.out, (size_t)om * a.out_row + on, v * gate + resid);
 }
 
+// 4 consecutive columns c.. of output row r (N % 8 == 0: in range as a whole), sa the row's scale
+template <int DT>
+__device__ __forceinline__ void finish4(const GemmI8Args& a, int r, int c, float sa, i32x4_t acc) {
+  const f32x4_t sw = load4<DT_F32>(a.w_s, c);
+  f32x4_t v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = (float)acc[e] * sa * sw[e];
+  if (a.bias) v += load4<DT>(a.bias, c);
+  if (a.gelu) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = gelu_tanh_f(v[e]);
+  }
+  if (a.gate) v *= load4<DT_F32>(a.gate, (size_t)((r + a.row0) / a.gate_rows) * a.gate_ld + c);
+  if (a.resid) v += load4<DT>(a.resid, (size_t)r * a.resid_row + c);
+  const size_t o = (size_t)r * a.out_row + c;
+  if (DT == DT_BF16) *reinterpret_cast<u32x2_t*>(reinterpret_cast<uint16_t*>(a.out) + o) = u32x2_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+  else *reinterpret_cast<f32x4_t*>(reinterpret_cast<float*>(a.out) + o) = v;
+}
+
 // Few rows: 16 x 16 tile, operands straight from memory, the NW waves of a workgroup on interleaved blocks of 128 k;
 // their sums meet in LDS.  Bound by the latency of the loads: M = 16, N = 8192, K = 2048 6.4 us; groups of four blocks
 // whatever is left, the rest clamped to the row's start, took 9.9.  16 waves were no faster (7.4; N = 2048,
@@ -272,22 +291,73 @@ __global__ __launch_bounds__(NW * 64) void k_gemm_i8_dir(GemmI8Args a) {
 #pragma unroll
   for (int i = 1; i < NW; ++i) acc += red[i][lane];
   const int r = m0 + l16, c = n0 + 4 * g;
-  if (r >= a.M || c >= a.N) return;   // N % 8 == 0: 4 columns are in range as a whole
-  const float sa = a.a_s[r];
-  const f32x4_t sw = load4<DT_F32>(a.w_s, c);
-  f32x4_t v;
+  if (r < a.M && c < a.N) finish4<DT>(a, r, c, a.a_s[r], acc);
+}
+
+// The same for up to 16 rows in a float type: every workgroup puts them in 8 bits for itself, into LDS, while its first
+// pieces of W are on their way.  M = 4, N = 512, K = 512 2.6 us for 4.2 with a launch before; N = 2048, K = 2048 4.4 for 5.6.
+constexpr int kOwnRows = 16;
+size_t own_lds(int M, int K) { return (size_t)M * ((K + 127) / 128 * 128 + 16); }
+template <int DA, int DT>
+__global__ __launch_bounds__(512) void k_gemm_i8_own(GemmI8Args a) {
+  constexpr int NW = 8, U = 4;
+  extern __shared__ __attribute__((aligned(16))) uint8_t rows[];   // [M][pitch]: zeros past K
+  __shared__ i32x4_t red[NW][64];
+  __shared__ float scales[kOwnRows];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l16 = lane & 15, g = lane >> 4, n0 = blockIdx.x * 16;
+  const int Kp = (a.K + 127) / 128 * 128, pitch = Kp + 16, nk = Kp / kQBlock;
+  const int m = l16 < a.M ? l16 : 0, n = n0 + l16 < a.N ? n0 + l16 : n0;   // past the matrix: never stored
+  const uint8_t* pw = a.w + (size_t)n * a.w_row;
+  u32x4_t w[U][2];
+  auto request = [&](int b0) __attribute__((always_inline)) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = (float)acc[e] * sa * sw[e];
-  if (a.bias) v += load4<DT>(a.bias, c);
-  if (a.gelu) {
+    for (int u = 0; u < U; ++u)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = gelu_tanh_f(v[e]);
+      for (int h = 0; h < 2; ++h) {   // chunks past K read the row's start, which is in bounds, and meet zeros
+        const int k = (b0 + NW * u) * kQBlock + g * 16 + h * 64;
+        if (b0 + NW * u < nk) w[u][h] = *reinterpret_cast<const u32x4_t*>(pw + (k < a.K ? k : 0));
+      }
+  };
+  request(wave);
+  for (int r = wave; r < a.M; r += NW) {
+    uint32_t top = 0;
+    for (int k = lane * 8; k < a.K; k += 512) {
+      float v[8];
+      load8<DA>(a.a, (size_t)r * a.a_row + k, v);
+      top = top_bits<8>(v, top);
+    }
+    const I8Scale q(top64(top));
+    if (lane == 0) scales[r] = q.s;
+    for (int k = lane * 8; k < Kp; k += 512) {
+      u32x2_t x = {0, 0};
+      if (k < a.K) {
+        float v[8];
+        load8<DA>(a.a, (size_t)r * a.a_row + k, v);   // from the caches
+        x = i8_pack8(v, q);
+      }
+      *reinterpret_cast<u32x2_t*>(rows + r * pitch + k) = x;
+    }
   }
-  if (a.gate) v *= load4<DT_F32>(a.gate, (size_t)((r + a.row0) / a.gate_rows) * a.gate_ld + c);
-  if (a.resid) v += load4<DT>(a.resid, (size_t)r * a.resid_row + c);
-  const size_t o = (size_t)r * a.out_row + c;
-  if (DT == DT_BF16) *reinterpret_cast<u32x2_t*>(reinterpret_cast<uint16_t*>(a.out) + o) = u32x2_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-  else *reinterpret_cast<f32x4_t*>(reinterpret_cast<float*>(a.out) + o) = v;
+  __syncthreads();
+  i32x4_t acc = {0, 0, 0, 0};
+  for (int b0 = wave; b0 < nk; b0 += NW * U) {
+    if (b0 != wave) request(b0);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (b0 + NW * u >= nk) break;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        acc = mfma_i8(w[u][h], *reinterpret_cast<const u32x4_t*>(rows + m * pitch + (b0 + NW * u) * kQBlock + g * 16 + h * 64), acc);
+    }
+  }
+  red[wave][lane] = acc;
+  __syncthreads();
+  if (wave) return;
+#pragma unroll
+  for (int i = 1; i < NW; ++i) acc += red[i][lane];
+  const int c = n0 + 4 * g;
+  if (l16 < a.M && c < a.N) finish4<DT>(a, l16, c, scales[l16], acc);
 }
 
 // ---------------------------------------------------------------- large grids: two wave groups in turn
@@ -766,6 +836,18 @@ namespace {
 I8Plan tail_plan(const I8Plan& p, int M, int N, int K) { return best_of(M - p.head, N, K, false).plan; }
 size_t part_bytes(const I8Plan& p, int M, int N) { return p.splits > 1 ? (size_t)p.splits * M * N * 4 : 0; }
 
+// Whether a call of few rows in a float type puts them in 8 bits in the product's own launch: while a wavefront's rows are
+// short (M = 16, N = 2048, K = 2048 6.3 us for 6.1 with a launch before, 4 rows of K = 8192 14.5 for 10.4), and what the
+// workgroups read of them together is little (M = 8, N = 8192, K = 2048 8.0 us for 8.2, 16 rows 10.6 for 8.7)
+bool own_rows(int a_dtype, int M, int N, int K) {
+  return a_dtype != DT_I8 && M <= kOwnRows && (M + 7) / 8 * K <= 4608 && (int64_t)M * K * ((N + 15) / 16) <= 1 << 23;
+}
+
+template <int DA, int DT>
+void launch_own(const GemmI8Args& a, hipStream_t s) {
+  FF_LAUNCH((k_gemm_i8_own<DA, DT>), (unsigned)((a.N + 15) / 16), 512, own_lds(a.M, a.K), s, a);
+}
+
 template <int DA, int DT>
 void launch_vec(const GemmI8Args& a, hipStream_t s) {
   const size_t lds = (size_t)a.M * ((a.K + 1023) / 1024 * 1024);
@@ -795,7 +877,7 @@ hipError_t launch_i8(const GemmI8Args& a, const I8Plan& p, hipStream_t s) {
 size_t gemm_i8_workspace(int a_dtype, int out_dtype, int M, int N, int K) {
   if (M <= 0) return 0;
   const I8Plan p = gemm_i8_plan(out_dtype, M, N, K);
-  if (p.kernel == I8_VEC) return 0;
+  if (p.kernel == I8_VEC || own_rows(a_dtype, M, N, K)) return 0;
   return rows_bytes(a_dtype, M, K) + (p.head < M ? part_bytes(tail_plan(p, M, N, K), M - p.head, N) : part_bytes(p, M, N));
 }
 
@@ -808,6 +890,11 @@ hipError_t gemm_i8(int a_dtype, int out_dtype, const GemmI8Args& a0, hipStream_t
     if (a_dtype == DT_I8) bf16 ? launch_vec<DT_I8, DT_BF16>(a, s) : launch_vec<DT_I8, DT_F32>(a, s);
     else if (a_dtype == DT_BF16) bf16 ? launch_vec<DT_BF16, DT_BF16>(a, s) : launch_vec<DT_BF16, DT_F32>(a, s);
     else bf16 ? launch_vec<DT_F32, DT_BF16>(a, s) : launch_vec<DT_F32, DT_F32>(a, s);
+    return hipGetLastError();
+  }
+  if (own_rows(a_dtype, a.M, a.N, a.K)) {
+    if (a_dtype == DT_BF16) bf16 ? launch_own<DT_BF16, DT_BF16>(a, s) : launch_own<DT_BF16, DT_F32>(a, s);
+    else bf16 ? launch_own<DT_F32, DT_BF16>(a, s) : launch_own<DT_F32, DT_F32>(a, s);
     return hipGetLastError();
   }
   if (a_dtype != DT_I8) {

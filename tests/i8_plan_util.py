@@ -29,6 +29,10 @@ PRODUCTS = [
     ((1, 520, 65552), (T64, 8, 1)),
     ((3, 8, 16), (DIR, 1, 3)),
     ((2, 40, 32784), (T64, 8, 2)),
+    ((16, 136, 2304), (DIR, 1, 16)),
+    ((8, 2056, 4608), (DIR, 1, 8)),
+    ((11, 72, 1040), (DIR, 1, 11)),
+    ((16, 2056, 2320), (DIR, 1, 16)),
     ((130, 264, 144), (DIR, 1, 130)),
     ((33, 1160, 1152), (DIR, 1, 33)),
     ((300, 72, 48), (T64, 1, 300)),

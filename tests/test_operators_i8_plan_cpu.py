@@ -19,13 +19,14 @@ def test_every_kernel_split_and_tail_is_reached():
 
 @pytest.mark.parametrize("shape,plan", P.PRODUCTS)
 def test_workspaces(shape, plan):
-    """Partial sums where K is split, of the rows that are; rows that the call puts in 8 bits, but for one or two."""
+    """Partial sums where K is split, of the rows that are; rows that the call puts in 8 bits, but for few short ones."""
     M, N, K = shape
+    own = M <= 16 and -(-M // 8) * K <= 4608 and M * K * -(-N // 16) <= 1 << 23
     kernel, splits, head = plan
     if head < M:
         splits, head = P.product(M - head, N, K)[1], M - head
     part = splits * head * N * 4 if splits > 1 else 0
     up = lambda n: -(-n // 256) * 256  # noqa: E731
-    for a, rows in ((abi.FF_I8, 0), (abi.FF_BF16, 0 if kernel == P.VEC else up(M * K) + up(4 * M))):
+    for a, rows in ((abi.FF_I8, 0), (abi.FF_BF16, None if kernel == P.VEC or own else up(M * K) + up(4 * M))):
         d = abi.ff_gemm_i8_desc(M=M, N=N, K=K, a_dtype=a, out_dtype=abi.FF_BF16, gelu=0, gate_rows=0, a_row=K, w_row=K, out_row=N, resid_row=N, gate_ld=0)
-        assert abi.ff_gemm_i8_workspace_bytes(d) == rows + part
+        assert abi.ff_gemm_i8_workspace_bytes(d) == (0 if rows is None else rows + part)

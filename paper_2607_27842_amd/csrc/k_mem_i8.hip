@@ -74,10 +74,12 @@ __global__ __launch_bounds__(kThreads) void k_draft_i8(TermsI8 t, const void* u,
   }
 }
 
-// Verify and replace (Eq. 3-5) on that draft: what k_verify does, with the same two-stage sums
+// Verify and replace (Eq. 3-5) on that draft: what k_verify does, with the same two-stage sums; a workgroup that has a
+// sample to itself finishes it.
 template <int DT, bool RES, int NT>
 __global__ __launch_bounds__(kThreads) void k_verify_i8(TermsI8 t, const void* u, const void* __restrict__ hf, void* hout, Forward fw,
-                                                        size_t n, size_t blocks, float* __restrict__ partials) {
+                                                        size_t n, size_t blocks, float* __restrict__ partials, float eps,
+                                                        float* __restrict__ rel) {
   __shared__ float red[2][kThreads / 64];
   const size_t base = (size_t)blockIdx.y * n, s0 = (size_t)blockIdx.y * blocks, q0 = s0 * kI8Block;
   float num = 0.f, den = 0.f;
@@ -105,9 +107,15 @@ __global__ __launch_bounds__(kThreads) void k_verify_i8(TermsI8 t, const void* u
   if ((threadIdx.x & 63) == 0) { red[0][threadIdx.x >> 6] = num; red[1][threadIdx.x >> 6] = den; }
   __syncthreads();
   if (threadIdx.x == 0) {
+    num = (red[0][0] + red[0][1]) + (red[0][2] + red[0][3]);
+    den = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
     float* p = partials + ((size_t)blockIdx.y * gridDim.x + blockIdx.x) * 2;
-    p[0] = (red[0][0] + red[0][1]) + (red[0][2] + red[0][3]);
-    p[1] = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
+    if (gridDim.x > 1) {
+      p[0] = num;
+      p[1] = den;
+    } else if (rel) {
+      rel[blockIdx.y] = num / (den + eps);
+    }
   }
 }
 
@@ -157,10 +165,11 @@ hipError_t draft_i8(int dtype, const TermsI8& t, const void* u, void* hd, int B,
 hipError_t verify_i8(int dtype, const TermsI8& t, const void* u, const void* hf, void* hout, const Forward& fw, int B, size_t n,
                      float eps, float* rel, float* partials, hipStream_t s) {
   const size_t blocks = i8_blocks(n);
-  const dim3 grid(groups_for(n), B);
-  FF_BY_TERMS(k_verify_i8, u != nullptr, t, u, hf, hout, fw, n, blocks, partials);
+  // four turns of one workgroup take less than a second launch
+  const dim3 grid(n <= 4 * kThreads * kPer ? 1 : groups_for(n), B);
+  FF_BY_TERMS(k_verify_i8, u != nullptr, t, u, hf, hout, fw, n, blocks, partials, eps, rel);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !rel) return e;
+  if (e != hipSuccess || !rel || grid.x == 1) return e;
   return verify_finish(partials, B, grid.x, eps, rel, s);
 }
 #undef FF_BY_TERMS

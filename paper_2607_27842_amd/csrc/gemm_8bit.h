@@ -17,9 +17,10 @@ template <int DT> struct Raw8;
 template <> struct Raw8<DT_BF16> {
   typedef u32x4_t type;
   __device__ __forceinline__ static type load(const void* p, size_t i) { return *reinterpret_cast<const u32x4_t*>(reinterpret_cast<const uint16_t*>(p) + i); }
+  __device__ __forceinline__ static float at(const type& w, int e) { return __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16); }
   __device__ __forceinline__ static void add(type w, float* v) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] += __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+    for (int e = 0; e < 8; ++e) v[e] += at(w, e);
   }
 };
 template <> struct Raw8<DT_F32> {
@@ -28,9 +29,10 @@ template <> struct Raw8<DT_F32> {
     const f32x4_t* q = reinterpret_cast<const f32x4_t*>(reinterpret_cast<const float*>(p) + i);
     return type{{q[0], q[1]}};
   }
+  __device__ __forceinline__ static float at(const type& w, int e) { return w.x[e / 4][e % 4]; }
   __device__ __forceinline__ static void add(const type& w, float* v) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] += w.x[e / 4][e % 4];
+    for (int e = 0; e < 8; ++e) v[e] += at(w, e);
   }
 };
 

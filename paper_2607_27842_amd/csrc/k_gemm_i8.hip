@@ -25,18 +25,30 @@ __device__ __forceinline__ i32x16_t mfma_i8(u32x4_t a, u32x4_t b, i32x16_t c) {
 }
 
 // ---------------------------------------------------------------- epilogue
-// Activation and gate of 8 columns c.. of row r, on the sums times both scales and the bias
-template <int DT>
-__device__ __forceinline__ void act_gate(const GemmI8Args& a, int r, int c, float (&v)[8]) {
-  if (a.gelu) {
+// Results of V columns from their sums, written out so that every kernel rounds alike: a row's results depend neither on
+// the other rows nor on the kernel that the call's sizes choose.  Absent parts: bias and resid 0, gate 1.
+template <int V>
+__device__ __forceinline__ void results(const GemmI8Args& a, const int (&sum)[V], float sa, const float (&sw)[V], const float (&bias)[V],
+                                        const float (&gate)[V], const float (&resid)[V], float (&v)[V]) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = gelu_tanh_f(v[e]);
+  for (int e = 0; e < V; ++e) v[e] = fmaf((float)sum[e] * sa, sw[e], bias[e]);
+  if (a.gelu) {   // a branch around all of them: as a choice for each, GELU is computed where nothing asks for it
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = gelu_tanh_f(v[e]);
   }
-  if (a.gate) {
-    float g[8];
-    load8<DT_F32>(a.gate, (size_t)((uint32_t)(r + a.row0) / (uint32_t)a.gate_rows) * a.gate_ld + c, g);
+  if (a.gate || a.resid) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] *= g[e];
+    for (int e = 0; e < V; ++e) v[e] = fmaf(v[e], gate[e], resid[e]);
+  }
+}
+template <int V>
+__device__ __forceinline__ void load_gate(const GemmI8Args& a, int r, int c, float (&g)[V]) {
+#pragma unroll
+  for (int e = 0; e < V; ++e) g[e] = 1.f;
+  if (a.gate) {
+    const size_t at = (size_t)((uint32_t)(r + a.row0) / (uint32_t)a.gate_rows) * a.gate_ld + c;
+#pragma unroll
+    for (int e = 0; e < V; e += 4) St<DT_F32>::load(a.gate, at + e, g + e);
   }
 }
 
@@ -96,11 +108,12 @@ __device__ __forceinline__ void epilogue(const GemmI8Args& a, int r0, int c0, in
       const i32x4_t x1 = *reinterpret_cast<const i32x4_t*>(lds + sum_at<WN>(p * RPP + pr, pc + 4));
       const int ri = i * RB + p * RPP;   // + pr, below 64 more than the multiple of 64 that it lies behind
       const float sr = __shfl(sa[ri / 64], ri % 64 + pr, 64);
-      float v[8];
+      float v[8], gate[8], resid[8];
+      load_gate(a, min(r, a.M - 1), cl, gate);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = fmaf((float)(e < 4 ? x0[e & 3] : x1[e & 3]) * sr, sw[e], bias[e]);
-      act_gate<DT>(a, min(r, a.M - 1), cl, v);
-      if (a.resid) Raw8<DT>::add(res[i & 1][p], v);
+      for (int e = 0; e < 8; ++e) resid[e] = a.resid ? Raw8<DT>::at(res[i & 1][p], e) : 0.f;
+      const int sum[8] = {x0[0], x0[1], x0[2], x0[3], x1[0], x1[1], x1[2], x1[3]};
+      results<8>(a, sum, sr, sw, bias, gate, resid, v);
       if (r < a.M && c < a.N) store8<DT>(a.out, (size_t)r * a.out_row + c, v);
     }
   }
@@ -211,37 +224,32 @@ __global__ __launch_bounds__(256) void k_gemm_i8_vec(GemmI8Args a) {
       }
     }
   }
-  float v = 0.f;
+  int sum = 0;
 #pragma unroll
   for (int m = 0; m < MR; ++m)
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const int s = lanes_sum(acc[m][r]);
-      if (lane == m * R + r) v = (float)s;
+      if (lane == m * R + r) sum = s;
     }
   if (!mine) return;
-  v = v * sa * sw + bias;
-  if (a.gelu) v = gelu_tanh_f(v);
-  St<DT>::st1(a.out, (size_t)om * a.out_row + on, v * gate + resid);
+  float v[1];
+  results<1>(a, {sum}, sa, {sw}, {bias}, {gate}, {resid}, v);
+  St<DT>::st1(a.out, (size_t)om * a.out_row + on, v[0]);
 }
 
 // 4 consecutive columns c.. of output row r (N % 8 == 0: in range as a whole), sa the row's scale
 template <int DT>
 __device__ __forceinline__ void finish4(const GemmI8Args& a, int r, int c, float sa, i32x4_t acc) {
-  const f32x4_t sw = load4<DT_F32>(a.w_s, c);
-  f32x4_t v;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = (float)acc[e] * sa * sw[e];
-  if (a.bias) v += load4<DT>(a.bias, c);
-  if (a.gelu) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = gelu_tanh_f(v[e]);
-  }
-  if (a.gate) v *= load4<DT_F32>(a.gate, (size_t)((r + a.row0) / a.gate_rows) * a.gate_ld + c);
-  if (a.resid) v += load4<DT>(a.resid, (size_t)r * a.resid_row + c);
+  const f32x4_t none = {0.f, 0.f, 0.f, 0.f}, s4 = load4<DT_F32>(a.w_s, c), b4 = a.bias ? load4<DT>(a.bias, c) : none;
+  const f32x4_t r4 = a.resid ? load4<DT>(a.resid, (size_t)r * a.resid_row + c) : none;
+  float gate[4], v[4];
+  load_gate(a, r, c, gate);
+  results<4>(a, {acc[0], acc[1], acc[2], acc[3]}, sa, {s4[0], s4[1], s4[2], s4[3]}, {b4[0], b4[1], b4[2], b4[3]}, gate,
+             {r4[0], r4[1], r4[2], r4[3]}, v);
   const size_t o = (size_t)r * a.out_row + c;
   if (DT == DT_BF16) *reinterpret_cast<u32x2_t*>(reinterpret_cast<uint16_t*>(a.out) + o) = u32x2_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-  else *reinterpret_cast<f32x4_t*>(reinterpret_cast<float*>(a.out) + o) = v;
+  else *reinterpret_cast<f32x4_t*>(reinterpret_cast<float*>(a.out) + o) = f32x4_t{v[0], v[1], v[2], v[3]};
 }
 
 // Few rows: 16 x 16 tile, operands straight from memory, the NW waves of a workgroup on interleaved blocks of 128 k;
@@ -750,21 +758,14 @@ __global__ __launch_bounds__(256) void k_gemm_i8_join(GemmI8Args a, int splits) 
     s[0] += p[0];
     s[1] += p[1];
   }
-  float v[8], x[8];
-  const float sa = a.a_s[r];
-  float bias[8];
+  float v[8], sw[8], bias[8], resid[8], gate[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) bias[e] = 0.f;
-  load8<DT_F32>(a.w_s, c, x);
+  for (int e = 0; e < 8; ++e) bias[e] = resid[e] = 0.f;
+  load8<DT_F32>(a.w_s, c, sw);
   if (a.bias) load8<DT>(a.bias, c, bias);
-#pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = fmaf((float)s[e / 4][e % 4] * sa, x[e], bias[e]);
-  act_gate<DT>(a, r, c, v);
-  if (a.resid) {
-    load8<DT>(a.resid, (size_t)r * a.resid_row + c, x);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] += x[e];
-  }
+  if (a.resid) load8<DT>(a.resid, (size_t)r * a.resid_row + c, resid);
+  load_gate(a, r, c, gate);
+  results<8>(a, {s[0][0], s[0][1], s[0][2], s[0][3], s[1][0], s[1][1], s[1][2], s[1][3]}, a.a_s[r], sw, bias, gate, resid, v);
   store8<DT>(a.out, (size_t)r * a.out_row + c, v);
 }
 

@@ -72,3 +72,29 @@ def test_two_streams_at_once(K):
                 I.gemm_call(x, None, w, w_s, out=o, ws=k)
     torch.cuda.synchronize()
     assert torch.equal(outs[0], want) and torch.equal(outs[1], want)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("rows", ["i8", "float"])
+def test_a_row_does_not_depend_on_the_others(dtype, rows):
+    """The first rows' bits at every number of rows, whatever kernel it takes."""
+    need_gpu()
+    g = O.gen(5)
+    N, K, most = 2056, 1168, 3000
+    x = O.randn((most, K), g, dtype).cuda()
+    q, s = I.quant_call(x)
+    w, w_s = I.quantise(O.randn((N, K), g, std=1 / math.sqrt(K)))
+    w, w_s = w.cuda(), w_s.cuda()
+    b, r, gate = O.randn((N,), g, dtype).cuda(), O.randn((most, N), g, dtype).cuda(), O.randn((1, N), g).cuda()
+    first, seen = None, set()
+    for M in (1, 2, 3, 16, 40, 200, 520, 1000, 2500, 3000):
+        seen.add(P.product(M, N, K)[0])
+        a = (x[:M], None) if rows == "float" else (q[:M], s[:M])
+        got = I.gemm_call(*a, w, w_s, b, True, gate, M, r[:M], dtype)
+        first = got[:1] if first is None else first
+        assert torch.equal(got[:1], first), M
+        if M > 3:
+            assert torch.equal(got[1:3], three[1:3]), M
+        elif M == 3:
+            three = got
+    assert {P.VEC, P.DIR, P.T64, P.T64X128, P.T128} <= seen, seen

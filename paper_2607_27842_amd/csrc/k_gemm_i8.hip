@@ -14,14 +14,9 @@ namespace ff {
 namespace {
 
 typedef int i32x4_t __attribute__((ext_vector_type(4)));
-typedef int i32x16_t __attribute__((ext_vector_type(16)));
 
 __device__ __forceinline__ i32x4_t mfma_i8(u32x4_t a, u32x4_t b, i32x4_t c) {
   return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4_t, a), __builtin_bit_cast(i32x4_t, b), c, 0, 0, 0);
-}
-
-__device__ __forceinline__ i32x16_t mfma_i8(u32x4_t a, u32x4_t b, i32x16_t c) {
-  return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4_t, a), __builtin_bit_cast(i32x4_t, b), c, 0, 0, 0);
 }
 
 // ---------------------------------------------------------------- epilogue
@@ -64,7 +59,7 @@ template <int WN> constexpr int sum_words(int rows) { return rows * (WN == 64 ? 
 // Rows r0 .. r0 + RB NB - 1, columns c0 .. c0 + WN - 1 of a wavefront: put(i) lays RB rows of sums at a time into
 // the wave's own LDS region, and they come back as 8-column pieces, so that
 // every load and store of bias, gate, residual and output is 16 bytes wide and covers whole row segments (in
-// the MFMA layout each store would put 8 bytes into each of 16 or 32 rows).  N % 8 == 0: a piece is in range as
+// the MFMA layout each store would put 8 bytes into each of 16 rows).  N % 8 == 0: a piece is in range as
 // a whole.  The caller has retired all waves' reads of what the region overlays.
 template <int DT, int WN, int RB, int NB, class F>
 __device__ __forceinline__ void epilogue(const GemmI8Args& a, int r0, int c0, int* lds, F&& put) {
@@ -371,8 +366,8 @@ __global__ __launch_bounds__(512) void k_gemm_i8_own(GemmI8Args a) {
 // ---------------------------------------------------------------- large grids: two wave groups in turn
 // 256 x 256 tile, a stage of 128 k, 8 waves in two groups of four, one wave of each group per SIMD; a stage has
 // four phases, one per 32 rows of a wave's 128 x 64 block.  A phase is a memory part (fragment reads,
-// DMA) and 8 MFMAs of 32 x 32 x 32, with a barrier after each; the second group runs half a phase behind, so that
-// on every SIMD one wave's MFMAs (256 cycles) cover the other's reads and DMA.
+// DMA) and 16 MFMAs, with a barrier after each; the second group runs half a phase behind, so that on every SIMD one
+// wave's MFMAs (256 cycles) cover the other's reads and DMA.
 //
 // Operands: 64-row pieces of 8 KB, each filled by one DMA instruction per wave, in two buffers per operand.  Phase
 // p of stage k issues, in this order:
@@ -380,12 +375,13 @@ __global__ __launch_bounds__(512) void k_gemm_i8_own(GemmI8Args a) {
 // and reads: phase 0 all B and A0 of stage k, phases 1-3 A1-A3.  So a piece's slot is refilled no earlier than
 // one phase after its last read.
 // K % 128 != 0: the last stage's chunks past K are out of the resource's range and load zeros.
-// What bounds it: with random operands the card's power limit (the same cycles on zeros, at a higher clock, take 0.65 of the
-// time at K = 8192, where MFMAs are busy 73 % of the cycles), then the epilogue, which one workgroup a CU leaves
-// uncovered.  M = 14336, N = 8192, K = 2048 (7 rounds of 256 tiles) 230 us, 2.09 POP/s, with bias and GELU 260; 210
-// and 231 without the stores (a measurement only); 8192 x 8192 x 8192 441 us, 2.49 POP/s.  A workgroup that walks
-// over tiles and requests the next one's first stages before its epilogue took 240 us: its stores hold the waits for the
-// next tile's operands.
+// What bounds it: with random operands the card's power limit (the same cycles on zeros, at a higher clock, took 0.65 of the
+// time at K = 8192 in 32 x 32 x 32 MFMAs), then the epilogue, which one workgroup a CU leaves uncovered.  So what an
+// MFMA moves counts: 16 x 16 x 64 pass 8 KB of operands and sums through the registers where 32 x 32 x 32 pass 10 for the
+// same products, and two in a row on the same sums less again.  M = 14336, N = 8192, K = 2048 (7 rounds of 256 tiles)
+// 215 us, 2.24 POP/s (32 x 32 x 32 236, 16 x 16 x 64 with the sums in turn 218), 8192 x 8192 x 8192 394, 2.79 POP/s (437,
+// 400); M = 14566 with bias and GELU 249 (274, 255).  A workgroup that walks over tiles and requests the next one's first
+// stages before its epilogue took 240 us for 230 then: its stores hold the waits for the next tile's operands.
 constexpr int kPPIssue[4][3] = {{3, -1, -1}, {0, 4, 5}, {1, 6, -1}, {2, 7, -1}};   // A0-A3, B0-B3
 // How many of a wave's DMAs may be outstanding at the end of phase p of a stage with `left` stages
 // after it (2: two or more), so that what phase p + 1 reads has landed.
@@ -438,38 +434,44 @@ __global__ __launch_bounds__(512) void k_gemm_i8_pp(GemmI8Args a) {
   }
   const bool cut = (int)ch >= a.K - (nk - 1) * kQBlock;   // this lane's chunk of the last stage lies past K
 #define FF_DMA(rs, vo, dst, kb) __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, FF_AS3(lds + (dst) + wave * 1024), 16, vo, kb, 0, 0)
-  i32x16_t acc[4][2];
+  i32x4_t acc[8][4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < 8; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
-  // lane l of a fragment: row l % 32, 16-byte chunk 2 s + l / 32 of its 128 (s: the MFMA's 32 k); columns 16 .. 31 of a B
-  // fragment stand in the next piece
+    for (int j = 0; j < 4; ++j) acc[i][j] = i32x4_t{0, 0, 0, 0};
   const uint32_t lds0 = (uint32_t)(uintptr_t)((__attribute__((address_space(3))) const void*)lds);
-  const int fr = lane & 31, fh = lane >> 5;
-  uint32_t rda[4], rdb[4];   // fragment addresses, current buffers
+  const int fr = lane & 15, fh = lane >> 4;
+  uint32_t rda[2], rdb[2];
 #pragma unroll
-  for (int s = 0; s < 4; ++s) {
-    const uint32_t c = ((2 * s + fh) ^ ((fr >> 1) & 7)) * 16;
+  for (int s = 0; s < 2; ++s) {
+    const uint32_t c = ((4 * s + fh) ^ (fr >> 1)) * 16;
     rda[s] = lds0 + (mw * 32 + fr) * RB + c;
-    rdb[s] = lds0 + OFFB + (fr >> 4) * PC + (nw * 16 + (fr & 15)) * RB + c;
+    rdb[s] = lds0 + OFFB + (nw * 16 + fr) * RB + c;
   }
-  u32x4_t fa[4], fb[2][4];
+  u32x4_t fa[2][2], fb[4][2];
   int kb = 0, ca = 0, cb = 0;   // this stage's byte offset along K, and its buffers
 #define FF_RDA(off)                                                                               \
   do {                                                                                            \
-    _Pragma("unroll") for (int s = 0; s < 4; ++s) fa[s] = __builtin_bit_cast(u32x4_t, lds_rd128_at<(off)>(rda[s])); \
+    _Pragma("unroll") for (int s = 0; s < 2; ++s) {                                               \
+      fa[0][s] = __builtin_bit_cast(u32x4_t, lds_rd128_at<(off)>(rda[s]));                        \
+      fa[1][s] = __builtin_bit_cast(u32x4_t, lds_rd128_at<(off) + 16 * RB>(rda[s]));              \
+    }                                                                                             \
   } while (0)
 #define FF_MEM_END() asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory")
 #define FF_MMA(q)                                                                                   \
   do {                                                                                              \
-    _Pragma("unroll") for (int s = 0; s < 4; ++s) FF_TIE(fa[s]);                                    \
+    _Pragma("unroll") for (int s = 0; s < 2; ++s) {                                                 \
+      FF_TIE(fa[0][s]);                                                                             \
+      FF_TIE(fa[1][s]);                                                                             \
+    }                                                                                               \
     __builtin_amdgcn_sched_barrier(0);                                                              \
     __builtin_amdgcn_s_setprio(1);                                                                  \
-    _Pragma("unroll") for (int s = 0; s < 4; ++s)                                                   \
-      _Pragma("unroll") for (int u = 0; u < 2; ++u) acc[q][u] = mfma_i8(fb[u][s], fa[s], acc[q][u]); \
+    _Pragma("unroll") for (int t = 0; t < 2; ++t)                                                   \
+      _Pragma("unroll") for (int u = 0; u < 4; ++u)                                                 \
+        _Pragma("unroll") for (int s = 0; s < 2; ++s) {                                                \
+          acc[2 * (q) + t][u] = mfma_i8(fb[u][s], fa[t][s], acc[2 * (q) + t][u]);                   \
+          __builtin_amdgcn_sched_barrier(0);                                                        \
+        }                                                                                           \
     __builtin_amdgcn_s_setprio(0);                                                                  \
     __builtin_amdgcn_sched_barrier(0);                                                              \
     asm volatile("s_barrier" ::: "memory");                                                         \
@@ -480,17 +482,17 @@ __global__ __launch_bounds__(512) void k_gemm_i8_pp(GemmI8Args a) {
     const int oa = BUFA - ca, ob = BUFB - cb;
     // phase 0
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < 4; ++u)
 #pragma unroll
-      for (int s = 0; s < 4; ++s) fb[u][s] = __builtin_bit_cast(u32x4_t, lds_rd128_off(rdb[s], u * 2 * PC));
+      for (int s = 0; s < 2; ++s) fb[u][s] = __builtin_bit_cast(u32x4_t, lds_rd128_off(rdb[s], u * PC));
     FF_RDA(0);
     if (k1) FF_DMA(ra, voa[3], 3 * PC + oa, kb + RB);
     wait_vm<pp_vm(0, LEFT)>();
     FF_MEM_END();
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < 4; ++u)
 #pragma unroll
-      for (int s = 0; s < 4; ++s) FF_TIE(fb[u][s]);
+      for (int s = 0; s < 2; ++s) FF_TIE(fb[u][s]);
     FF_MMA(0);
     // phase 1
     FF_RDA(1 * PC);
@@ -514,7 +516,7 @@ __global__ __launch_bounds__(512) void k_gemm_i8_pp(GemmI8Args a) {
     // phase 3
     FF_RDA(3 * PC);
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
+    for (int s = 0; s < 2; ++s) {
       rda[s] += oa - ca;
       rdb[s] += ob - cb;
     }
@@ -563,13 +565,10 @@ __global__ __launch_bounds__(512) void k_gemm_i8_pp(GemmI8Args a) {
   // every wave's LDS reads and DMA ended before the last barrier
   int* const own = reinterpret_cast<int*>(lds) + wave * sum_words<WN>(32);
   epilogue<DT, WN, 32, 4>(a, m0 + mw * 128, n0 + nw * WN, own, [&](int i) __attribute__((always_inline)) {
-    // lane l: row l % 32, columns 8 j + 4 (l / 32) + 0..3
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        *reinterpret_cast<i32x4_t*>(own + sum_at<WN>(fr, 32 * u + 8 * j + 4 * fh)) =
-            i32x4_t{acc[i][u][4 * j], acc[i][u][4 * j + 1], acc[i][u][4 * j + 2], acc[i][u][4 * j + 3]};
+      for (int u = 0; u < 4; ++u) *reinterpret_cast<i32x4_t*>(own + sum_at<WN>(16 * t + fr, 16 * u + 4 * fh)) = acc[2 * i + t][u];
   });
 #endif
 }
@@ -781,7 +780,7 @@ size_t rows_bytes(int a_dtype, int M, int K) { return a_dtype == DT_I8 ? 0 : ((s
 //   M 64 N 2048 K 8192: 64 x 64 14.4 us, with 2 / 4 / 8 splits of K 12.5 / 11.1 / 12.6; 16 x 16 16.6
 //   M 256 N 6144 K 2048: 64 x 128 9.0 us, 128 x 64 9.0, 64 x 64 9.8, 128 x 128 11.9; M 1024 N 2048 K 8192: 21.7, 22.4, 26.3, 28.6
 //   M 512 N 8192 K 2048: 128 x 128 12.9 us, 64 x 64 17.0, 256 x 256 25.1
-//   M 4608 N 6144 K 2048: 256 x 256 59.0 us, 128 x 128 77.7, 64 x 64 97.0
+//   M 4608 N 6144 K 2048: 256 x 256 56.3 us, 128 x 128 77.7, 64 x 64 97.0
 double us_dir(double t, double nk) { return 2.2 + fmax(t * nk * 0.45e-3, 0.115 * nk); }
 double us_64(double t, double nk) {
   if (t <= 256) return 3.5 + (0.17 + 0.06 * t / 256) * nk;
@@ -796,7 +795,7 @@ double us_128(double t, double nk) { return t <= 256 ? 5.5 + (0.37 + 0.10 * t / 
 // rounds of all 256 CUs run at the power limit, a last one with fewer at a higher clock
 double us_256(double t, double nk) {
   const double full = floor(t / 256), last = t / 256 - full, f = last * last;
-  return 4.0 + full * (1.6 * nk + 6.5) + (last > 0 ? (0.95 + 0.65 * f) * nk + 1.0 + 5.5 * f : 0.0);
+  return 4.0 + full * (1.43 * nk + 6.8) + (last > 0 ? (0.90 + 0.53 * f) * nk + 1.0 + 5.8 * f : 0.0);
 }
 
 struct Timed { I8Plan plan; double us; };
@@ -816,7 +815,7 @@ Timed best_of(int M, int N, int K, bool cut) {
   if (nk < 3) return b;
   take(I8_TILE256, 1, M, us_256(t256, nk));
   // Rows behind whole rounds of 256 x 256 tiles in a launch of their own, with the tile that suits them (M = 14566,
-  // N = 8192, K = 2048, whose eighth round has 32 tiles: 240 us for 257)
+  // N = 8192, K = 2048, whose eighth round has 32 tiles: 240 us for 257 with 32 x 32 x 32 MFMAs)
   const int per = (N + 255) / 256;
   const int head = (int)(floor(t256 / 256) * 256) / per * 256;
   if (cut && head > 0 && head < M) take(I8_TILE256, 1, head, us_256((double)tiles(head, N, 256), nk) + best_of(M - head, N, K, false).us - 0.5);

@@ -579,8 +579,11 @@ __global__ __launch_bounds__(512) void k_gemm_i8_pp(GemmI8Args a) {
 // Per block a wave has a memory slot (its fragments) and a matrix slot (the MFMAs, and behind each a DMA of the block
 // NS ahead into the ring slot just read), each ended by a barrier; the second group runs one slot
 // behind, one wave of each group per SIMD.  The two groups' sums meet in LDS: each finishes half of the rows.
-// What bounds it: the chain of LDS reads, waits and barriers (64 x 64: 0.17 us a block of K with one workgroup on a CU, 0.36
-// a pair of blocks with two), and with all CUs what the caches deliver (128 x 128: 0.5 us a block).
+// What bounds it: the operands' way into LDS, 70 to 95 GB/s a CU in every tile (64 x 64: 0.17 us a block of K with one
+// workgroup on a CU, 0.36 a pair of blocks with two; 64 x 128: 0.27; 128 x 128: 0.38, 0.5 with all CUs busy).  Neither a
+// third block in the ring (M = 256, N = 6144, K = 2048 8.6 us for 8.4) nor half the LDS reads help: waves that take halves of
+// a block's k for the whole column half, and join their sums at the end, took 9.2 us for 8.7 there, 15.1 for 14.0 at
+// M = 512, N = 8192.  Requesting what the epilogue needs before the first DMA: 13.9 for 13.5.
 template <int DT, int BM, int BN, int NS>
 __global__ __launch_bounds__(512) void k_gemm_i8_two(GemmI8Args a, int splits) {
 #ifdef __HIP_DEVICE_COMPILE__   // the host pass needs the launch stub only
@@ -648,7 +651,9 @@ __global__ __launch_bounds__(512) void k_gemm_i8_two(GemmI8Args a, int splits) {
 #pragma unroll
       for (int j = 0; j < PER; ++j) issue1(i, i, j);
     }
-  wait_vm<0>();
+  // the first block has landed (a wait for all of them: 8.7 us for 8.4 at M = 256, N = 6144, K = 2048)
+  if (mine >= NS) wait_vm<(NS - 1) * PER>();
+  else wait_vm<0>();
   asm volatile("s_barrier" ::: "memory");
   if (grp) asm volatile("s_barrier" ::: "memory");   // the second group runs one slot behind
   int slot = 0;
@@ -783,15 +788,15 @@ size_t rows_bytes(int a_dtype, int M, int K) { return a_dtype == DT_I8 ? 0 : ((s
 //   M 4608 N 6144 K 2048: 256 x 256 56.3 us, 128 x 128 77.7, 64 x 64 97.0
 double us_dir(double t, double nk) { return 2.2 + fmax(t * nk * 0.45e-3, 0.115 * nk); }
 double us_64(double t, double nk) {
-  if (t <= 256) return 3.5 + (0.17 + 0.06 * t / 256) * nk;
-  if (t <= 512) return 4.3 + (0.30 + 0.04 * (t - 256) / 256) * nk;   // two workgroups on some CUs
-  return 3.0 + ceil(t / 256) / 2 * (0.36 * nk + 1.3);
+  if (t <= 256) return 3.2 + (0.17 + 0.06 * t / 256) * nk;
+  if (t <= 512) return 4.0 + (0.30 + 0.04 * (t - 256) / 256) * nk;   // two workgroups on some CUs
+  return 2.7 + ceil(t / 256) / 2 * (0.36 * nk + 1.3);
 }
 double us_join(int splits, double outputs) { return 1.2 + splits * (0.55 + 0.5e-6 * outputs); }
 double us_64x128(double t, double nk) {
-  return t <= 256 ? 3.8 + t / 256 + (0.235 + 0.05 * t / 256) * nk : 3.0 + ceil(t / 256) * (0.285 * nk + 2.4);
+  return t <= 256 ? 3.5 + t / 256 + (0.235 + 0.05 * t / 256) * nk : 2.7 + ceil(t / 256) * (0.285 * nk + 2.4);
 }
-double us_128(double t, double nk) { return t <= 256 ? 5.5 + (0.37 + 0.10 * t / 256) * nk : 3.0 + ceil(t / 256) * (0.5 * nk + 2.2); }
+double us_128(double t, double nk) { return t <= 256 ? 5.2 + (0.37 + 0.10 * t / 256) * nk : 2.7 + ceil(t / 256) * (0.5 * nk + 2.2); }
 // rounds of all 256 CUs run at the power limit, a last one with fewer at a higher clock
 double us_256(double t, double nk) {
   const double full = floor(t / 256), last = t / 256 - full, f = last * last;

@@ -375,8 +375,8 @@ __global__ __launch_bounds__(512) void k_gemm_i8_own(GemmI8Args a) {
 // and reads: phase 0 all B and A0 of stage k, phases 1-3 A1-A3.  So a piece's slot is refilled no earlier than
 // one phase after its last read.
 // K % 128 != 0: the last stage's chunks past K are out of the resource's range and load zeros.
-// What bounds it: with random operands the card's power limit (the same cycles on zeros, at a higher clock, took 0.65 of the
-// time at K = 8192 in 32 x 32 x 32 MFMAs), then the epilogue, which one workgroup a CU leaves uncovered.  So what an
+// What bounds it: with random operands the card's power limit (the same cycles on zeros, at a higher clock, take 0.7 of the
+// time at K = 8192), then the epilogue, which one workgroup a CU leaves uncovered.  So what an
 // MFMA moves counts: 16 x 16 x 64 pass 8 KB of operands and sums through the registers where 32 x 32 x 32 pass 10 for the
 // same products, and two in a row on the same sums less again.  M = 14336, N = 8192, K = 2048 (7 rounds of 256 tiles)
 // 215 us, 2.24 POP/s (32 x 32 x 32 236, 16 x 16 x 64 with the sums in turn 218), 8192 x 8192 x 8192 394, 2.79 POP/s (437,

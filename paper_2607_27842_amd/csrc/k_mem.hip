@@ -169,7 +169,6 @@ __device__ __forceinline__ void block_sum2(float& a, float& b) {
   }
 }
 
-constexpr int kMaxVerifyBlocks = 2048;  // partial-sum blocks per sample
 
 // Verify + replace (Eq. 3-5): rebuild the draft from the same incoming u, accumulate
 // sum|h_d - h_f| and sum|h_f| for this sample, and forward h_f (FeatFix) or h_d (Verify).

@@ -9,7 +9,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kPer = 8;   // values a lane; 16 lanes hold a block
-constexpr int kMaxGroups = 2048;
+constexpr int kMaxGroups = kMaxVerifyBlocks;   // a sample; the verify pass keeps two sums of each
 
 // Delta = h - u (or h) in fp32, then its blocks.  Values past the sample's end are written as zeros.  A sample's size is a
 // multiple of 8.

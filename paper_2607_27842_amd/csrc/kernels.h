@@ -271,6 +271,7 @@ hipError_t draft_sum(int dtype, const Terms& t, void* x, size_t E, hipStream_t s
 // stride-th row (token) / channel of a sample with C channels and the draft elsewhere.
 enum { FWD_DRAFT = 0, FWD_EXACT = 1, FWD_TOKENS = 2, FWD_CHANNELS = 3 };
 struct Forward { int kind, stride, C; };
+constexpr int kMaxVerifyBlocks = 2048;  // partial-sum blocks per sample
 size_t verify_partials_floats(int B);
 hipError_t verify(int dtype, const Terms& t, const void* u, const void* hf, void* hout, const Forward& fw,
                   int B, size_t Eb, float eps, float* rel_l1, float* partials, hipStream_t s);

@@ -96,7 +96,7 @@ __global__ __launch_bounds__(256) void k_quant_i8_long(QuantI8Args a) {
 }
 
 // As many walks as the card holds at once, each of W of about 6144 wavefronts (k_branch_norm, 14566 x 2048: 2048 walks
-// instead of 1536, 54.7 us for 50.4, as some start late; 3072 50.7, 8192 53.2).
+// instead of 1536, 54.7 us for 50.4, as some start late; twice as many 50.7, 8192 53.2).
 int walks_for(int rows, int W) { return rows < 6144 / W ? rows : 6144 / W; }
 
 template <int DT, int W, int U>

@@ -98,3 +98,37 @@ def test_a_row_does_not_depend_on_the_others(dtype, rows):
         elif M == 3:
             three = got
     assert {P.VEC, P.DIR, P.T64, P.T64X128, P.T128} <= seen, seen
+
+
+@pytest.mark.parametrize("shape", [(5000, 2600, 400), (7268, 2056, 8208)])
+def test_rows_of_large_products_in_small_ones(shape):
+    """The same bits whether a row is among thousands, behind the whole rounds of tiles, or one of 130 or two."""
+    need_gpu()
+    M, N, K = shape
+    plan = P.product(M, N, K)
+    assert plan[0] == P.T256
+    g = O.gen(9)
+    q, s = I.quant_call(O.randn((M, K), g, BF).cuda())
+    w, w_s = I.quantise(O.randn((N, K), g, std=1 / math.sqrt(K)))
+    w, w_s, b, r = w.cuda(), w_s.cuda(), O.randn((N,), g, BF).cuda(), O.randn((M, N), g, BF).cuda()
+    gate = O.randn((M, N), g).cuda()
+    full = I.gemm_call(q, s, w, w_s, b, True, gate, 1, r)
+    for at in (0, 700, min(plan[2], M - 130), M - 130):
+        for n in (130, 2):
+            got = I.gemm_call(q[at:at + n], s[at:at + n].clone(), w, w_s, b, True, gate[at:at + n], 1, r[at:at + n])
+            assert torch.equal(got, full[at:at + n]), (at, n)
+
+
+@pytest.mark.parametrize("into", ["x", "branch"])
+@pytest.mark.parametrize("rows,C", [(1700, 2056), (6500, 264)])
+def test_branch_in_place_on_long_walks(rows, C, into):
+    """The sum in the place of what it is formed from, while the next rows are on their way."""
+    need_gpu()
+    g = O.gen(6)
+    x, z, v = O.randn((rows, C), g, BF).cuda(), O.randn((rows, C), g, BF).cuda(), O.randn((3, C), g).cuda()
+    new = lambda: torch.empty(rows, C, dtype=BF, device="cuda")  # noqa: E731
+    how = dict(post="rms", gate=v, pre="layer", scale=v, shift=v, mod_rows=-(-rows // 3))
+    t, y, y2 = new(), new(), new()
+    I.branch_call(x, branch=z, **how, sum=t, y=y)
+    I.branch_call(x, branch=z, **how, sum=x if into == "x" else z, y=y2)
+    assert torch.equal(x if into == "x" else z, t) and torch.equal(y2, y)

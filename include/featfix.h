@@ -577,7 +577,8 @@ typedef struct {
 /* out [M, N] <- act(a_s[m] w_s[n] sum_k a[m, k] w[n, k] + bias[n]) gate[m / gate_rows][n] + resid[m, n]
  * A [M, K] with scales a_s [M] (NULL unless a_dtype is FF_I8), W [N, K] int8 with w_s [N].  The sum is exact
  * (integers below 2^31; values of -128 are taken as they are); then fp32, one rounding to out_dtype, the same for
- * any M: a row's results depend neither on the other rows nor on their number.  bias [N],
+ * any M: a row's results depend neither on the other rows nor on their number.  Sum and scales overflow only where their
+ * product is beyond fp32.  bias [N],
  * gate (fp32 vectors of N: a block's per-sample gate) and resid [M, N] may be NULL; out may be resid
  * itself at the same pitch.  ws: at least ff_gemm_i8_workspace_bytes(d) bytes (NULL if that is 0: it
  * holds the rows that the call puts in 8 bits, and partial sums where few rows meet a long K).

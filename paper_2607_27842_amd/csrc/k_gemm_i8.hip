@@ -22,11 +22,19 @@ __device__ __forceinline__ i32x4_t mfma_i8(u32x4_t a, u32x4_t b, i32x4_t c) {
 // ---------------------------------------------------------------- epilogue
 // Results of V columns from their sums, written out so that every kernel rounds alike: a row's results depend neither on
 // the other rows nor on the kernel that the call's sizes choose.  Absent parts: bias and resid 0, gate 1.
-template <int V>
+// sum sa may be beyond fp32 (sums are below 2^31) though sw brings it back.  FAR: where sa is from 2^96 on, the line is formed at
+// 2^-32 of its size, which changes no rounding of results from 2^-94 on.
+__device__ __forceinline__ bool is_far(float sa) { return fabsf(sa) >= 0x1p96f; }
+template <bool FAR, int V>
 __device__ __forceinline__ void results(const GemmI8Args& a, const int (&sum)[V], float sa, const float (&sw)[V], const float (&bias)[V],
                                         const float (&gate)[V], const float (&resid)[V], float (&v)[V]) {
+  if (FAR && __builtin_expect(is_far(sa), 0)) {
 #pragma unroll
-  for (int e = 0; e < V; ++e) v[e] = fmaf((float)sum[e] * sa, sw[e], bias[e]);
+    for (int e = 0; e < V; ++e) v[e] = fmaf((float)sum[e] * 0x1p-32f * sa, sw[e], bias[e] * 0x1p-32f) * 0x1p32f;
+  } else {
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = fmaf((float)sum[e] * sa, sw[e], bias[e]);
+  }
   if (a.gelu) {   // a branch around all of them: as a choice for each, GELU is computed where nothing asks for it
 #pragma unroll
     for (int e = 0; e < V; ++e) v[e] = gelu_tanh_f(v[e]);
@@ -55,6 +63,33 @@ __device__ __forceinline__ int sum_at(int row, int col) {
   else return row * (WN + 4) + col;
 }
 template <int WN> constexpr int sum_words(int rows) { return rows * (WN == 64 ? WN : WN + 4); }
+
+// Those of the rows r0 .. r0 + rows - 1 whose scale is as large as FAR's (values from 10^31 on), columns c0 .. c0 + WN - 1, formed
+// again from the operands, a column a lane.  As slow as that is, the epilogue's loop needs no registers for them.
+template <int DT, int WN>
+__device__ __forceinline__ void far_rows(const GemmI8Args& a, int r0, int rows, int c0) {
+  const int lane = threadIdx.x & 63, c = c0 + lane % WN;
+  if (c >= a.N) return;
+  const uint8_t* const pw = a.w + (size_t)c * a.w_row;
+#pragma unroll 1
+  for (int r = r0 + lane / WN; r < min(r0 + rows, a.M); r += 64 / WN) {
+    const float sa = a.a_s[r];
+    if (!is_far(sa)) continue;
+    const uint8_t* const pa = static_cast<const uint8_t*>(a.a) + (size_t)r * a.a_row;
+    int sum = 0;
+#pragma unroll 1
+    for (int k = 0; k < a.K; k += 16) {
+      const u32x4_t x = *reinterpret_cast<const u32x4_t*>(pa + k), w = *reinterpret_cast<const u32x4_t*>(pw + k);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum = __builtin_amdgcn_sdot4((int)w[e], (int)x[e], sum, false);
+    }
+    const float bias = a.bias ? St<DT>::ld1(a.bias, c) : 0.f, resid = a.resid ? St<DT>::ld1(a.resid, (size_t)r * a.resid_row + c) : 0.f;
+    const float gate = a.gate ? a.gate[(size_t)((uint32_t)(r + a.row0) / (uint32_t)a.gate_rows) * a.gate_ld + c] : 1.f;
+    float v[1];
+    results<true>(a, {sum}, sa, {a.w_s[c]}, {bias}, {gate}, {resid}, v);
+    St<DT>::st1(a.out, (size_t)r * a.out_row + c, v[0]);
+  }
+}
 
 // Rows r0 .. r0 + RB NB - 1, columns c0 .. c0 + WN - 1 of a wavefront: put(i) lays RB rows of sums at a time into
 // the wave's own LDS region, and they come back as 8-column pieces, so that
@@ -108,10 +143,15 @@ __device__ __forceinline__ void epilogue(const GemmI8Args& a, int r0, int c0, in
 #pragma unroll
       for (int e = 0; e < 8; ++e) resid[e] = a.resid ? Raw8<DT>::at(res[i & 1][p], e) : 0.f;
       const int sum[8] = {x0[0], x0[1], x0[2], x0[3], x1[0], x1[1], x1[2], x1[3]};
-      results<8>(a, sum, sr, sw, bias, gate, resid, v);
-      if (r < a.M && c < a.N) store8<DT>(a.out, (size_t)r * a.out_row + c, v);
+      results<false>(a, sum, sr, sw, bias, gate, resid, v);
+      if (r < a.M && c < a.N && !is_far(sr)) store8<DT>(a.out, (size_t)r * a.out_row + c, v);
     }
   }
+  // Scales as large as FAR's.  A branch for each row above, in place of the mask, takes 215 us for 211 (14336 x 8192 x 2048).
+  bool far = false;
+#pragma unroll
+  for (int i = 0; i < NS; ++i) far |= is_far(sa[i]);
+  if (__builtin_expect(__any(far), 0)) far_rows<DT, WN>(a, r0, RB * NB, c0);
 }
 
 // ---------------------------------------------------------------- one and two rows
@@ -229,7 +269,7 @@ __global__ __launch_bounds__(256) void k_gemm_i8_vec(GemmI8Args a) {
     }
   if (!mine) return;
   float v[1];
-  results<1>(a, {sum}, sa, {sw}, {bias}, {gate}, {resid}, v);
+  results<true>(a, {sum}, sa, {sw}, {bias}, {gate}, {resid}, v);
   St<DT>::st1(a.out, (size_t)om * a.out_row + on, v[0]);
 }
 
@@ -240,7 +280,7 @@ __device__ __forceinline__ void finish4(const GemmI8Args& a, int r, int c, float
   const f32x4_t r4 = a.resid ? load4<DT>(a.resid, (size_t)r * a.resid_row + c) : none;
   float gate[4], v[4];
   load_gate(a, r, c, gate);
-  results<4>(a, {acc[0], acc[1], acc[2], acc[3]}, sa, {s4[0], s4[1], s4[2], s4[3]}, {b4[0], b4[1], b4[2], b4[3]}, gate,
+  results<true>(a, {acc[0], acc[1], acc[2], acc[3]}, sa, {s4[0], s4[1], s4[2], s4[3]}, {b4[0], b4[1], b4[2], b4[3]}, gate,
              {r4[0], r4[1], r4[2], r4[3]}, v);
   const size_t o = (size_t)r * a.out_row + c;
   if (DT == DT_BF16) *reinterpret_cast<u32x2_t*>(reinterpret_cast<uint16_t*>(a.out) + o) = u32x2_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
@@ -769,7 +809,7 @@ __global__ __launch_bounds__(256) void k_gemm_i8_join(GemmI8Args a, int splits) 
   if (a.bias) load8<DT>(a.bias, c, bias);
   if (a.resid) load8<DT>(a.resid, (size_t)r * a.resid_row + c, resid);
   load_gate(a, r, c, gate);
-  results<8>(a, {s[0][0], s[0][1], s[0][2], s[0][3], s[1][0], s[1][1], s[1][2], s[1][3]}, a.a_s[r], sw, bias, gate, resid, v);
+  results<true>(a, {s[0][0], s[0][1], s[0][2], s[0][3], s[1][0], s[1][1], s[1][2], s[1][3]}, a.a_s[r], sw, bias, gate, resid, v);
   store8<DT>(a.out, (size_t)r * a.out_row + c, v);
 }
 

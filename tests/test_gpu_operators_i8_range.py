@@ -1,0 +1,55 @@
+"""Products of 8-bit integers and norms between branches near the ends of what fp32 holds."""
+import math
+
+import pytest
+import torch
+
+import i8_util as I
+import op_util as O
+from gpu_util import need_gpu
+
+pytestmark = pytest.mark.gpu
+BF, F32, I8 = torch.bfloat16, torch.float32, torch.int8
+TYPES = pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+
+
+def cycle(values, n):
+    return torch.tensor(values).repeat(-(-n // len(values)))[:n]
+
+
+# every kernel: one and two rows, few rows, K split, the tiles, rows behind whole rounds of large tiles
+@TYPES
+@pytest.mark.parametrize("rows", ["i8", "float"])
+@pytest.mark.parametrize("parts", [False, True], ids=["bias", "gate_and_residual_in_place"])
+@pytest.mark.parametrize("M,N,K", [(1, 520, 272), (2, 24, 1040), (4, 200, 272), (16, 136, 2304), (33, 1160, 1152), (130, 2056, 8208),
+                                   (520, 2056, 1168), (1100, 2056, 2064), (5000, 2600, 400), (7176, 2056, 400)])
+def test_large_scales_of_rows_meet_small_ones_of_columns(dtype, parts, rows, M, N, K):
+    """A sum times its row's scale is beyond fp32, the product with its column's scale is not: rows of 8-bit integers with such
+    scales, and rows of values near the type's largest.  Columns with large scales have infinities, but zeros where the sum
+    is zero; rows and columns of ordinary scales are as ever."""
+    need_gpu()
+    g = O.gen(M + N + K)
+    a = torch.randint(-128, 128, (M, K), generator=g).to(I8)
+    if M > 1:
+        a[M // 2] = 0
+    a_s = cycle([3e38, 1.0, 1e35, 2.0 ** 96, 1.5 * 2.0 ** 97, 1e-30, 2.0 ** 95], M)
+    w = torch.randint(-128, 128, (N, K), generator=g).to(I8)
+    w_s = cycle([1e-36, 2.0 ** -120, 1e-40, 1e-38, 1.0, 1e-33], N)
+    w_s[-3] = 1e38
+    bias, resid = O.randn((N,), g, dtype), O.randn((M, N), g, dtype) if parts else None
+    per = max(1, 2 * M // 5 - 3)
+    gate = torch.stack([cycle([1.5, -2.0, 1.0, -1.25], N + i)[i:] for i in range(-(-M // per))]) if parts else None
+    out = resid.cuda() if parts else None
+    more = dict(gate=gate.cuda(), gate_rows=per, resid=out, out=out) if parts else {}
+    if rows == "i8":
+        got = I.gemm_call(a.cuda(), a_s.cuda(), w.cuda(), w_s.cuda(), bias.cuda(), dtype=dtype, **more)
+    else:
+        x = (a.float() * cycle([2e36, 1.0, 1e-3, 2.0 ** 100], M)[:, None]).to(dtype)
+        a, a_s = I.quantise(x)
+        got = I.gemm_call(x.cuda(), None, w.cuda(), w_s.cuda(), bias.cuda(), dtype=dtype, **more)
+    ref, tol = I.gemm_ref(a, a_s, w, w_s, bias, False, gate, per, resid, dtype)
+    far = torch.isinf(ref.float().to(dtype))
+    assert far.any() and not far.all()
+    ref[far] = math.inf * ref[far].sign()
+    tol[far] = 0.0
+    O.close(got, ref, tol, "gemm")

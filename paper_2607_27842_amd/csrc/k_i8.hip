@@ -142,32 +142,63 @@ __device__ __forceinline__ float over_row(float v, float* at, int wave) {
   return sum;
 }
 
-// v <- v normed.  Columns past the row hold zeros before and after.
-template <int W, int U>
-__device__ __forceinline__ void norm_row(float (&v)[U][8], const BranchArgs& a, int kind, int l, float* at, int wave) {
-  if (kind == NORM_NONE) return;
-  if (kind == NORM_LAYER) {
-    float sum = 0.f;
+template <int U>
+__device__ __forceinline__ float sum_of(const float (&v)[U][8]) {
+  float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < U; ++i)
+  for (int i = 0; i < U; ++i)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum += v[i][e];
-    const float mean = over_row<W>(sum, at, wave) / (float)a.C;
-#pragma unroll
-    for (int i = 0; i < U; ++i)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] = (l + 64 * W * i) * 8 < a.C ? v[i][e] - mean : 0.f;
-  }
+    for (int e = 0; e < 8; ++e) sum += v[i][e];
+  return sum;
+}
+template <int U>
+__device__ __forceinline__ float squares_of(const float (&v)[U][8]) {
   float ss = 0.f;
 #pragma unroll
   for (int i = 0; i < U; ++i)
 #pragma unroll
     for (int e = 0; e < 8; ++e) ss = fmaf(v[i][e], v[i][e], ss);
-  const float inv = 1.0f / sqrtf(over_row<W>(ss, at + W, wave) / (float)a.C + a.eps);
+  return ss;
+}
+template <int U>
+__device__ __forceinline__ void times(float (&v)[U][8], float by) {
 #pragma unroll
   for (int i = 0; i < U; ++i)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[i][e] *= inv;
+    for (int e = 0; e < 8; ++e) v[i][e] *= by;
+}
+
+// v <- v normed.  Columns past the row hold zeros before and after.  Sums that fp32 does not hold (squares beyond 2^128, or a mean that
+// v - mean could overflow with) are formed again from the row times 2^-80: values below 2^-46 of a row whose root mean square is above
+// 2^57 lose digits by that, results below 2^-103.  All of the row's lanes hold the same sums, so that they take these branches
+// together.  14566 x 2048 bf16 takes the same time with and without them, 4000 x 8192 77.5 us for 76.0.
+constexpr int kNormSums = 4;   // reductions at most
+template <int W, int U>
+__device__ __forceinline__ void norm_row(float (&v)[U][8], const BranchArgs& a, int kind, int l, float* at, int wave) {
+  if (kind == NORM_NONE) return;
+  float eps = a.eps, least = 0.f;
+  if (kind == NORM_LAYER) {
+    float sum = over_row<W>(sum_of<U>(v), at, wave);
+    if (__builtin_expect(!(fabsf(sum) < 0x1p100f), 0)) {
+      times<U>(v, 0x1p-80f);
+      eps = a.eps * 0x1p-80f * 0x1p-80f;
+      least = 0x1p-126f;   // for values all alike, where eps is gone as well
+      sum = over_row<W>(sum_of<U>(v), at + 2 * W, wave);
+    }
+    const float mean = sum / (float)a.C;
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] = (l + 64 * W * i) * 8 < a.C ? v[i][e] - mean : 0.f;
+  }
+  float ss = over_row<W>(squares_of<U>(v), at + W, wave);
+  if (__builtin_expect(!(ss < __builtin_inff()), 0)) {
+    times<U>(v, 0x1p-80f);
+    eps = a.eps * 0x1p-80f * 0x1p-80f;
+    ss = over_row<W>(squares_of<U>(v), at + 3 * W, wave);
+  }
+  const float square = ss / (float)a.C + eps;
+  times<U>(v, 1.0f / sqrtf(square < least ? least : square));
 }
 
 // What a row's columns are multiplied by and moved by, the same for all rows of a sample
@@ -205,7 +236,7 @@ __device__ __forceinline__ void load_vectors(const BranchArgs& k, size_t smp, in
 // workgroup 60.3, walks of neighbouring rows 54.1.  One row 3.6 us, a launch.
 template <int DT, int W, int U>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_branch_norm(BranchArgs a, int step) {
-  __shared__ float part[2][5 * W];   // a row's reductions have a place each, and rows in turn two sets
+  __shared__ float part[2][(2 * kNormSums + 1) * W];   // a row's reductions have a place each, and rows in turn two sets
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int l = W == 1 ? lane : (int)threadIdx.x;
   int row = (W == 1 ? blockIdx.x * 4 + wave : blockIdx.x);
@@ -221,15 +252,28 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_branch_norm(BranchArg
       if (a.branch) pz[i].load(a.branch, (size_t)r * a.branch_row + c);
     }
   };
-  constexpr bool kAhead = W * U <= 16;   // the widest rows need the registers
-  if (kAhead) request(row);
+  // The widest rows need the registers: their lanes keep what the second norm meets in LDS, each for itself (2000 x 16384 fp32
+  // 117.7 us; with all vectors in registers, some of which spill, 152.8; read again for each row 137).
+  constexpr bool kPark = W * U > 16;
+  __shared__ f32x4_t parked[kPark ? 4 * U : 1][kPark ? 64 * W : 1];
+  auto park = [&](Vectors<U>& v, bool back) __attribute__((always_inline)) {
+    if (!kPark) return;
+#pragma unroll
+    for (int i = 0; i < 4 * U; ++i) {
+      float* const at = (i & 2 ? v.s : v.p)[i / 4] + (i & 1) * 4;
+      f32x4_t& to = parked[i][l];
+      if (back) for (int e = 0; e < 4; ++e) at[e] = to[e];
+      else to = f32x4_t{at[0], at[1], at[2], at[3]};
+    }
+  };
+  request(row);
   Vectors<U> v;
   int smp = row / a.mod_rows, next = min((smp + 1) * (int64_t)a.mod_rows, (int64_t)a.rows);   // the next sample's first row
   load_vectors<DT, W, U>(a, smp, l, v);
+  park(v, false);
   for (;; row += step) {
     float* const at = part[turn++ & 1];
     float t[U][8], z[U][8];
-    if (!kAhead) request(row);
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       const bool in = (l + 64 * W * i) * 8 < a.C;
@@ -243,8 +287,9 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_branch_norm(BranchArg
       smp = row / a.mod_rows;
       next = min((smp + 1) * (int64_t)a.mod_rows, (int64_t)a.rows);
       load_vectors<DT, W, U>(a, smp, l, v);
+      park(v, false);
     }
-    if (kAhead && row + step < a.rows) request(row + step);
+    if (row + step < a.rows) request(row + step);
     if (a.branch) norm_row<W, U>(z, a, a.post, l, at, wave);
 #pragma unroll
     for (int i = 0; i < U; ++i) {
@@ -254,7 +299,8 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_branch_norm(BranchArg
       if (a.sum && c < a.C) store8<DT>(a.sum, (size_t)row * a.sum_row + c, t[i]);
     }
     if (a.y || a.q) {
-      norm_row<W, U>(t, a, a.pre, l, at + 2 * W, wave);
+      norm_row<W, U>(t, a, a.pre, l, at + kNormSums * W, wave);
+      park(v, true);
       uint32_t top = 0;
 #pragma unroll
       for (int i = 0; i < U; ++i) {
@@ -265,7 +311,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_branch_norm(BranchArg
         top = top_bits<8>(t[i], top);   // columns past C hold zeros
       }
       if (a.q) {
-        const I8Scale k(top_row<W>(top, at + 4 * W, wave));
+        const I8Scale k(top_row<W>(top, at + 2 * kNormSums * W, wave));
 #pragma unroll
         for (int i = 0; i < U; ++i) {
           const int c = (l + 64 * W * i) * 8;

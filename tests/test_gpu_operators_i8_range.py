@@ -53,3 +53,42 @@ def test_large_scales_of_rows_meet_small_ones_of_columns(dtype, parts, rows, M, 
     ref[far] = math.inf * ref[far].sign()
     tol[far] = 0.0
     O.close(got, ref, tol, "gemm")
+
+
+SIZES = [1e18, 1e19, 2e19, 1e25, 1e37, 3e38]
+
+
+def edge_rows(C, g, dtype):
+    """Rows of values up to each of SIZES, one with small values beside a single large one, one of a large mean (what
+    squares of its spread alone would not show), one of values all alike, an ordinary one."""
+    x = torch.rand((len(SIZES) + 4, C), generator=g, dtype=torch.float64) * 2 - 1
+    x[:len(SIZES)] *= torch.tensor(SIZES)[:, None]
+    x[len(SIZES)] *= 1e-3
+    x[len(SIZES), C // 2] = -1e30
+    x[len(SIZES) + 1] = 1e38 + 1e37 * x[len(SIZES) + 1]
+    x[len(SIZES) + 2] = 2.0 ** 100
+    return x.to(dtype)
+
+
+# one, two, four, eight and sixteen wavefronts a row, one and two pieces a lane
+@TYPES
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("C", [264, 1032, 2048, 4096, 8192, 16384])
+def test_norms_of_rows_whose_squares_leave_fp32(dtype, kind, C):
+    """Both places of a norm, each followed by the other's work.  The roundings are norm_ref's; a row of equal values of a power of
+    two has them as its mean, without any.  Such rows are summed at 2^-80 of their size, where a small value is off by half a
+    step of the least numbers, 2^-150: after the division by at least 2^57 2^-80, 2^-127 in the result, below 1e-37."""
+    need_gpu()
+    g = O.gen(C)
+    x = edge_rows(C, g, dtype)
+    rows = x.shape[0]
+    dx, zero = x.cuda(), torch.zeros_like(x).cuda()
+    y, t, q, s = torch.empty_like(dx), torch.empty_like(dx), torch.empty(rows, C, dtype=I8, device="cuda"), torch.empty(rows, device="cuda")
+    I.branch_call(dx, pre=kind, y=y, q=q, q_s=s)
+    v, e = I.norm_ref(x.double(), kind, 1e-6)
+    O.close(y, v, e + (O.HALF[dtype] + O.U) * (v.abs() + e) + 1e-37, "in front")
+    I.close_q(q, s, v, e)
+    I.branch_call(zero, dx, kind, sum=t, pre="rms", y=y)
+    O.close(t, v, e + (O.HALF[dtype] + O.U) * (v.abs() + e) + 1e-37, "behind")
+    v, e = I.norm_ref(t.cpu().double(), "rms", 1e-6)
+    O.close(y, v, e + (O.HALF[dtype] + O.U) * (v.abs() + e) + 1e-37, "behind and in front")

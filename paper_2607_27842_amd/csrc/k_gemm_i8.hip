@@ -619,7 +619,7 @@ __global__ __launch_bounds__(512) void k_gemm_i8_pp(GemmI8Args a) {
 // Per block a wave has a memory slot (its fragments) and a matrix slot (the MFMAs, and behind each a DMA of the block
 // NS ahead into the ring slot just read), each ended by a barrier; the second group runs one slot
 // behind, one wave of each group per SIMD.  The two groups' sums meet in LDS: each finishes half of the rows.
-// What bounds it: the operands' way into LDS, 70 to 95 GB/s a CU in every tile (64 x 64: 0.17 us a block of K with one
+// What bounds it: the operands' way into LDS, at 70 to 95 GB/s a CU in every tile, observed, without a cause found (64 x 64: 0.17 us a block of K with one
 // workgroup on a CU, 0.36 a pair of blocks with two; 64 x 128: 0.27; 128 x 128: 0.38, 0.5 with all CUs busy).  Neither a
 // third block in the ring (M = 256, N = 6144, K = 2048 8.6 us for 8.4) nor half the LDS reads help: waves that take halves of
 // a block's k for the whole column half, and join their sums at the end, took 9.2 us for 8.7 there, 15.1 for 14.0 at
@@ -820,12 +820,16 @@ long tiles(long M, long N, long t) { return ((M + t - 1) / t) * ((N + t - 1) / t
 size_t rows_bytes(int a_dtype, int M, int K) { return a_dtype == DT_I8 ? 0 : ((size_t)M * K + 255) / 256 * 256 + ((size_t)M * 4 + 255) / 256 * 256; }
 
 // The kernel of a shape by estimated time (us): fits to 60 shapes of 1 to 14566 rows, N and K of 256 to 8192, 8-bit rows,
-// bf16 out.  nk: blocks of K; t: tiles.  Examples, measured:
-//   M 16 N 8192 K 2048: 16 x 16 6.4 us, 64 x 64 6.8; M 64 N 2048: 5.6, 5.7; M 128 N 2048: 16, 5.8
-//   M 64 N 2048 K 8192: 64 x 64 14.4 us, with 2 / 4 / 8 splits of K 12.5 / 11.1 / 12.6; 16 x 16 16.6
-//   M 256 N 6144 K 2048: 64 x 128 9.0 us, 128 x 64 9.0, 64 x 64 9.8, 128 x 128 11.9; M 1024 N 2048 K 8192: 21.7, 22.4, 26.3, 28.6
-//   M 512 N 8192 K 2048: 128 x 128 12.9 us, 64 x 64 17.0, 256 x 256 25.1
-//   M 4608 N 6144 K 2048: 256 x 256 56.3 us, 128 x 128 77.7, 64 x 64 97.0
+// bf16 out, nothing behind the product.  nk: blocks of K; t: tiles.  Examples, measured with each kernel:
+//   M 16 N 8192 K 2048: 16 x 16 6.1 us, 64 x 64 6.6; M 64 N 2048: 5.6, 5.7; M 128 N 2048: 9.0, 5.7
+//   M 64 N 2048 K 8192: 64 x 64 14.1 us, with 2 / 4 / 8 splits of K 12.4 / 10.9 / 12.5; 16 x 16 16.6
+//   M 256 N 6144 K 2048: 64 x 128 8.4 us, 64 x 64 9.4, 128 x 128 11.4; M 1024 N 2048 K 8192: 21.4, 26.4, 28.1
+//   M 512 N 8192 K 2048: 128 x 128 13.5 us, 64 x 128 16.7, 64 x 64 17.5, 256 x 256 26.0
+//   M 4608 N 6144 K 2048: 256 x 256 55.8 us, 128 x 128 80.4, 64 x 64 95.4
+// Of 19 shapes of 16 to 14566 rows the choice is the fastest for 17; 256 x 256 tiles are taken where 128 x 128 ones are for M 2048
+// N 3456 K 1152 (20.1 us for 17.9) and M 700 N 8192 K 1024 (18.6 for 16.5).  fp32 outputs with bias, gate and residual, whose
+// epilogue the estimates do not know: the fastest for 16; 64 x 64 tiles would be for these two (27.1 us for 24.6, 25.1
+// for 20.0) and M 333 N 4096 K 1024 (8.4 for 8.0).
 double us_dir(double t, double nk) { return 2.2 + fmax(t * nk * 0.45e-3, 0.115 * nk); }
 double us_64(double t, double nk) {
   if (t <= 256) return 3.2 + (0.17 + 0.06 * t / 256) * nk;
@@ -870,7 +874,7 @@ Timed best_of(int M, int N, int K, bool cut) {
 }  // namespace
 
 I8Plan gemm_i8_plan(int out_dtype, int M, int N, int K) {
-  (void)out_dtype;
+  (void)out_dtype;   // both types by the fits to bf16's times
   if (M <= kVecRows && (size_t)M * ((K + 1023) / 1024 * 1024) <= kVecBytes) return I8Plan{I8_VEC, 1, M};
   return best_of(M, N, K, true).plan;
 }

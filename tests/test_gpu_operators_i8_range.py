@@ -55,6 +55,25 @@ def test_large_scales_of_rows_meet_small_ones_of_columns(dtype, parts, rows, M, 
     O.close(got, ref, tol, "gemm")
 
 
+
+@pytest.mark.parametrize("rows", ["i8", "float"])
+def test_a_row_with_a_large_scale_does_not_depend_on_the_others(rows):
+    """The first three rows' bits at every number of rows, whatever kernel it takes, among rows of large and small scales."""
+    need_gpu()
+    g = O.gen(11)
+    N, K, most = 2056, 1168, 3000
+    x = (torch.randint(-128, 128, (most, K), generator=g) * cycle([2e36, 1.0, 1e30, 1e-3], most)[:, None]).cuda()
+    q, s = I.quant_call(x)
+    w, w_s = I.quantise(O.randn((N, K), g))
+    w, w_s = w.cuda(), (w_s * 1e-30).cuda()
+    b, r, gate = O.randn((N,), g).cuda(), O.randn((most, N), g).cuda(), O.randn((1, N), g).cuda()
+    got = {}
+    for M in (1, 2, 3, 16, 40, 200, 520, 1000, 2500, 3000):
+        a = (x[:M], None) if rows == "float" else (q[:M], s[:M])
+        got[M] = I.gemm_call(*a, w, w_s, b, True, gate, M, r[:M], F32)
+        assert torch.isfinite(got[M]).all()
+        assert all(torch.equal(got[M][:n], got[n]) for n in got if n <= 3), M
+
 SIZES = [1e18, 1e19, 2e19, 1e25, 1e37, 3e38]
 
 

@@ -607,7 +607,7 @@ typedef struct {
  *     t = round_dtype(resid_scale x + g N_post(branch) post_gain),   g = gate or tanh(gate)
  *     v = N_pre(t) pre_gain (1 + scale) + shift
  * N: v / sqrt(mean(v^2) + eps) (FF_NORM_RMS), that of v less its mean (FF_NORM_LAYER), or v (FF_NORM_NONE); fp32.  A
- * row whose squares or sum leave fp32 is summed at 2^-80 of its size: results below 2^-103 lose digits, nothing else.
+ * row whose squares leave fp32 is summed at 2^-80 of its size: results below 2^-103 lose digits, nothing else.
  * branch (and post_gain, gate) NULL: t = round_dtype(resid_scale x).  The gains [C], gate, scale and shift (fp32
  * vectors of C) may be NULL: ones, and zeros for scale and shift.  sum (may be x or branch itself, at the same pitch)
  * receives t, y v rounded to dtype, q with q_s (NULL together) v as rows of 8-bit integers, from the

@@ -145,15 +145,6 @@ __device__ __forceinline__ float over_row(float v, float* at, int wave) {
 }
 
 template <int U>
-__device__ __forceinline__ float sum_of(const float (&v)[U][8]) {
-  float sum = 0.f;
-#pragma unroll
-  for (int i = 0; i < U; ++i)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sum += v[i][e];
-  return sum;
-}
-template <int U>
 __device__ __forceinline__ float squares_of(const float (&v)[U][8]) {
   float ss = 0.f;
 #pragma unroll
@@ -170,37 +161,36 @@ __device__ __forceinline__ void times(float (&v)[U][8], float by) {
     for (int e = 0; e < 8; ++e) v[i][e] *= by;
 }
 
-// v <- v normed.  Columns past the row hold zeros before and after.  Sums that fp32 does not hold (squares beyond 2^128, or a mean that
-// v - mean could overflow with) are formed again from the row times 2^-80: values below 2^-46 of a row whose root mean square is above
-// 2^57 lose digits by that, results below 2^-103.  All of the row's lanes hold the same sums, so that they take these branches
-// together.  14566 x 2048 bf16 takes the same time with and without them, 4000 x 8192 77.5 us for 76.0.
-constexpr int kNormSums = 4;   // reductions at most
+// v <- v normed.  Columns past the row hold zeros before and after.  Nothing on the way leaves fp32: the mean is formed from 2^-14 of
+// the values (C <= 2^14), and half of v - mean takes its place; a sum of squares that overflows is formed again from the row times
+// 2^-80, in a branch that all of the row's lanes take together, as they hold the same sum.  Powers of two change no rounding, but that
+// values below 2^-46 of a row whose root mean square is above 2^57 lose digits, results below 2^-103.  14566 x 2048 bf16 takes
+// the same time with and without that branch; another one behind the mean, 3000 x 6000 bf16, both LayerNorm, 59.8 us for 55.6.
+constexpr int kNormSums = 3;   // reductions at most
 template <int W, int U>
 __device__ __forceinline__ void norm_row(float (&v)[U][8], const BranchArgs& a, int kind, int l, float* at, int wave) {
   if (kind == NORM_NONE) return;
-  float eps = a.eps, least = 0.f;
+  float eps = a.eps;
   if (kind == NORM_LAYER) {
-    float sum = over_row<W>(sum_of<U>(v), at, wave);
-    if (__builtin_expect(!(fabsf(sum) < 0x1p100f), 0)) {
-      times<U>(v, 0x1p-80f);
-      eps = a.eps * 0x1p-80f * 0x1p-80f;
-      least = 0x1p-126f;   // for values all alike, where eps is gone as well
-      sum = over_row<W>(sum_of<U>(v), at + 2 * W, wave);
-    }
-    const float mean = sum / (float)a.C;
+    float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < U; ++i)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] = (l + 64 * W * i) * 8 < a.C ? v[i][e] - mean : 0.f;
+      for (int e = 0; e < 8; ++e) sum = fmaf(v[i][e], 0x1p-14f, sum);
+    const float half = over_row<W>(sum, at, wave) / (float)a.C * 0x1p13f;
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] = (l + 64 * W * i) * 8 < a.C ? fmaf(v[i][e], 0.5f, -half) : 0.f;
+    eps *= 0.25f;
   }
   float ss = over_row<W>(squares_of<U>(v), at + W, wave);
   if (__builtin_expect(!(ss < __builtin_inff()), 0)) {
     times<U>(v, 0x1p-80f);
-    eps = a.eps * 0x1p-80f * 0x1p-80f;
-    ss = over_row<W>(squares_of<U>(v), at + 3 * W, wave);
+    eps = eps * 0x1p-80f * 0x1p-80f;
+    ss = over_row<W>(squares_of<U>(v), at + 2 * W, wave);
   }
-  const float square = ss / (float)a.C + eps;
-  times<U>(v, 1.0f / sqrtf(square < least ? least : square));
+  times<U>(v, 1.0f / sqrtf(ss / (float)a.C + eps));
 }
 
 // What a row's columns are multiplied by and moved by, the same for all rows of a sample

@@ -79,13 +79,16 @@ SIZES = [1e18, 1e19, 2e19, 1e25, 1e37, 3e38]
 
 def edge_rows(C, g, dtype):
     """Rows of values up to each of SIZES, one with small values beside a single large one, one of a large mean (what
-    squares of its spread alone would not show), one of values all alike, an ordinary one."""
-    x = torch.rand((len(SIZES) + 4, C), generator=g, dtype=torch.float64) * 2 - 1
+    squares of its spread alone would not show), one of values all alike, an ordinary one, one whose values lie further from
+    their mean than fp32 reaches."""
+    x = torch.rand((len(SIZES) + 5, C), generator=g, dtype=torch.float64) * 2 - 1
     x[:len(SIZES)] *= torch.tensor(SIZES)[:, None]
     x[len(SIZES)] *= 1e-3
     x[len(SIZES), C // 2] = -1e30
     x[len(SIZES) + 1] = 1e38 + 1e37 * x[len(SIZES) + 1]
     x[len(SIZES) + 2] = 2.0 ** 100
+    x[len(SIZES) + 4] = 3e38 + 3e37 * x[len(SIZES) + 4]
+    x[len(SIZES) + 4, ::9] *= -1
     return x.to(dtype)
 
 

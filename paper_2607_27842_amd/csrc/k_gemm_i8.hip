@@ -619,11 +619,11 @@ __global__ __launch_bounds__(512) void k_gemm_i8_pp(GemmI8Args a) {
 // Per block a wave has a memory slot (its fragments) and a matrix slot (the MFMAs, and behind each a DMA of the block
 // NS ahead into the ring slot just read), each ended by a barrier; the second group runs one slot
 // behind, one wave of each group per SIMD.  The two groups' sums meet in LDS: each finishes half of the rows.
-// What bounds it: the operands' way into LDS, at 70 to 95 GB/s a CU in every tile, observed, without a cause found (64 x 64: 0.17 us a block of K with one
-// workgroup on a CU, 0.36 a pair of blocks with two; 64 x 128: 0.27; 128 x 128: 0.38, 0.5 with all CUs busy).  Neither a
-// third block in the ring (M = 256, N = 6144, K = 2048 8.6 us for 8.4) nor half the LDS reads help: waves that take halves of
-// a block's k for the whole column half, and join their sums at the end, took 9.2 us for 8.7 there, 15.1 for 14.0 at
-// M = 512, N = 8192.  Requesting what the epilogue needs before the first DMA: 13.9 for 13.5.
+// What bounds it: the operands' way into LDS, at 70 to 95 GB/s a CU in every tile, observed, without a cause found (64 x 64:
+// 0.17 us a block of K with one workgroup on a CU, 0.36 a pair of blocks with two; 64 x 128: 0.27; 128 x 128: 0.38, 0.5
+// with all CUs busy).  Neither a third block in the ring (M = 256, N = 6144, K = 2048 8.6 us for 8.4) nor half the LDS reads
+// help: waves that take halves of a block's k for the whole column half, and join their sums at the end, took 9.2 us for 8.7
+// there, 15.1 for 14.0 at M = 512, N = 8192.  Requesting what the epilogue needs before the first DMA: 13.9 for 13.5.
 template <int DT, int BM, int BN, int NS>
 __global__ __launch_bounds__(512) void k_gemm_i8_two(GemmI8Args a, int splits) {
 #ifdef __HIP_DEVICE_COMPILE__   // the host pass needs the launch stub only

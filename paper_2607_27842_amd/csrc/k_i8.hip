@@ -106,8 +106,8 @@ void launch_quant_walks(const QuantI8Args& a, hipStream_t s) {
   else FF_LAUNCH((k_quant_i8<DT, W, U>), walks, 64 * W, 0, s, a, walks);
 }
 
-// A row in registers: one unit a lane up to 2048 columns, two above, with as few wavefronts as that takes (8000 x 3000 bf16 13.4 us, with
-// one unit 14.2, with four 13.8; 4000 x 8192 17.8, 19.8, 18.4; 14566 x 1024 9.2, with two 9.4, with four 10.6).
+// A row in registers: one unit a lane up to 2048 columns, two above, with as few wavefronts as that takes (8000 x 3000
+// bf16 13.4 us, with one unit 14.2, with four 13.8; 4000 x 8192 17.8, 19.8, 18.4; 14566 x 1024 9.2, with two 9.4, with four 10.6).
 template <int DT>
 void launch_quant(const QuantI8Args& a, hipStream_t s) {
   const int units = a.C / 8;
@@ -161,11 +161,12 @@ __device__ __forceinline__ void times(float (&v)[U][8], float by) {
     for (int e = 0; e < 8; ++e) v[i][e] *= by;
 }
 
-// v <- v normed.  Columns past the row hold zeros before and after.  Nothing on the way leaves fp32: the mean is formed from 2^-14 of
-// the values (C <= 2^14), and half of v - mean takes its place; a sum of squares that overflows is formed again from the row times
-// 2^-80, in a branch that all of the row's lanes take together, as they hold the same sum.  Powers of two change no rounding, but that
-// values below 2^-46 of a row whose root mean square is above 2^57 lose digits, results below 2^-103.  14566 x 2048 bf16 takes
-// the same time with and without that branch; another one behind the mean, 3000 x 6000 bf16, both LayerNorm, 59.8 us for 55.6.
+// v <- v normed.  Columns past the row hold zeros before and after.  Nothing on the way leaves fp32: the mean is formed from
+// 2^-14 of the values (C <= 2^14), and half of v - mean takes its place; a sum of squares that overflows is formed again
+// from the row times 2^-80, in a branch that all of the row's lanes take together, as they hold the same sum.  Powers of
+// two change no rounding, but that values below 2^-46 of a row whose root mean square is above 2^57 lose digits, results below
+// 2^-103.  14566 x 2048 bf16 takes the same time with and without that branch; another one behind the mean, 3000 x 6000
+// bf16, both LayerNorm, 59.8 us for 55.6.
 constexpr int kNormSums = 3;   // reductions at most
 template <int W, int U>
 __device__ __forceinline__ void norm_row(float (&v)[U][8], const BranchArgs& a, int kind, int l, float* at, int wave) {
@@ -182,7 +183,7 @@ __device__ __forceinline__ void norm_row(float (&v)[U][8], const BranchArgs& a, 
     for (int i = 0; i < U; ++i)
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[i][e] = (l + 64 * W * i) * 8 < a.C ? fmaf(v[i][e], 0.5f, -half) : 0.f;
-    eps *= 0.25f;
+    eps = fmaxf(eps * 0.25f, 0x1p-149f);   // the least of all would be gone, and a row of zeros NaN
   }
   float ss = over_row<W>(squares_of<U>(v), at + W, wave);
   if (__builtin_expect(!(ss < __builtin_inff()), 0)) {
@@ -224,8 +225,8 @@ __device__ __forceinline__ void load_vectors(const BranchArgs& k, size_t smp, in
 // W wavefronts hold a row, U units of 8 columns a lane; a workgroup (or, W = 1, a wavefront) walks every step-th row.
 // The next row's values are requested before this row's sums meet, and the sample's vectors stay in registers
 // from row to row: read again for each row they are twice a bf16 row's own bytes, from L2.  Bound by memory: 14566 x 2048
-// bf16, both norms, gate, scale and shift, 47.9 to 50.4 us from run to run, 4.74 to 4.98 TB/s of the 5.0 that a large copy reaches; a row a
-// workgroup 60.3 for 50.4, walks of neighbouring rows 54.1.  One row 3.6 us, a launch.
+// bf16, both norms, gate, scale and shift, 47.9 to 50.4 us from run to run, 4.74 to 4.98 TB/s of the 5.0 that a large
+// copy reaches; a row a workgroup 60.3 for 50.4, walks of neighbouring rows 54.1.  One row 3.6 us, a launch.
 template <int DT, int W, int U>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_branch_norm(BranchArgs a, int step) {
   __shared__ float part[2][(2 * kNormSums + 1) * W];   // a row's reductions have a place each, and rows in turn two sets

@@ -114,3 +114,23 @@ def test_norms_of_rows_whose_squares_leave_fp32(dtype, kind, C):
     O.close(t, v, e + (O.HALF[dtype] + O.U) * (v.abs() + e) + 1e-37, "behind")
     v, e = I.norm_ref(t.cpu().double(), "rms", 1e-6)
     O.close(y, v, e + (O.HALF[dtype] + O.U) * (v.abs() + e) + 1e-37, "behind and in front")
+
+
+@TYPES
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("eps", [2.0 ** -149, 2.0 ** -126, 1e-20, 1e20, 3e38])
+def test_norms_with_any_eps(dtype, kind, eps):
+    """Rows of zeros stay zeros with the least eps there is; rows of order one are normed; with a large eps, beside rows whose squares
+    leave fp32, results are what is left of them (below 2^-103 with the digits that fp32 has there)."""
+    need_gpu()
+    g = O.gen(4)
+    for C in (264, 2048, 16384):
+        x = O.randn((5, C), g)
+        x[0], x[2], x[3] = 0.0, x[2] * 1e25, x[3] * 1e18
+        x = x.to(dtype)
+        dx = x.cuda()
+        y, q, s = torch.empty_like(dx), torch.empty(5, C, dtype=I8, device="cuda"), torch.empty(5, device="cuda")
+        I.branch_call(dx, pre=kind, y=y, q=q, q_s=s, eps=eps)
+        assert (y[0] == 0).all() and (q[0] == 0).all()
+        v, e = I.norm_ref(x.double(), kind, torch.tensor(eps).double())
+        O.close(y, v, e + (O.HALF[dtype] + O.U) * (v.abs() + e) + 1e-37, "y")
